@@ -240,6 +240,99 @@ int kvattn_kv_append(const void* k_new, const void* v_new, const int32_t* slot_m
                      int head_dim, int block_size, kv_dtype dtype, void* stream);
 
 /* ------------------------------------------------------------------------- */
+/* The cache in 8 bits: a layer whose K and V are e4m3 with a power of two for each
+ * block of tokens, kv head and K or V. It takes half a bf16 layer's bytes, so a
+ * decode step reads half and the same pool holds twice the tokens.
+ *
+ * A layer is num_blocks blocks of kvattn_fp8_block_bytes(num_kv_heads, head_dim)
+ * bytes (a multiple of 128; 0 for sizes not built), each
+ *   [2 (K=0, V=1)][num_kv_heads][block_size * head_dim] codes,
+ *   [num_kv_heads][2 (K, V)] exponent bytes,
+ *   padding that nobody reads.
+ * In a K tile token r, dim j is code (j / 16 * 16 + r) * 16 + j % 16; in a V tile code
+ * j / 64 * 1024 + r / 4 * 256 + j % 16 * 16 + j / 16 % 4 * 4 + r % 4. A tile's values are
+ * code * 2^(byte - 127), byte 10 .. 246. The block is whole in itself:
+ * kvattn_copy_blocks moves it (block_bytes as above), and the elastic pool holds it
+ * like any other. Block tables, lengths and slots are those of a bf16 layer.
+ *
+ * kvattn_kv_append_fp8: kvattn_kv_append for such a layer, same arguments, k_new and
+ * v_new in bf16 or fp32. The tokens of one block must stand next to each other in
+ * slot_mapping (a sequence's new tokens in order do). They are scaled together:
+ * with e the least exponent with |x| <= 448 * 2^e over their finite values in
+ * a kv head's K (or V), a call that writes slot 0 begins the block anew and its
+ * exponent is e (what other slots held has no meaning any more); any other call
+ * takes max(e, the block's exponent), and where that is larger the block's other codes
+ * are rounded to the new scale (exact but for those that leave e4m3's normal range, below
+ * 2^-14 of the largest value). Values are rounded to nearest even; NaN and
+ * infinities become NaN, finite values beyond 448 * 2^119 the largest code. Skipped
+ * slots, alignment and repeated slots as for kvattn_kv_append; a block whose tokens stand
+ * in several places of one call's list has unspecified contents.
+ * Supported: head_dim 64 and 128, block_size 16.
+ *
+ * kvattn_decode_fp8, kvattn_prefill_chunk_fp8: kvattn_decode and
+ * kvattn_prefill_chunk over such a layer: same arguments, workspaces (of the same
+ * size functions) and rules; dtype is the type of q and out and must be KV_BF16. The
+ * products are of bf16 (codes times their power of two are exact there), sums and
+ * softmax in fp32; the prefill's scale must be above zero. Supported: decode head_dim 64 and 128, prefill 128; block_size
+ * 16; num_q_heads / num_kv_heads in {1, 2, 4, 8}. */
+size_t kvattn_fp8_block_bytes(int num_kv_heads, int head_dim);
+
+int kvattn_kv_append_fp8(const void* k_new, const void* v_new, const int32_t* slot_mapping,
+                         void* kv_layer, int num_blocks, int num_tokens, int num_kv_heads,
+                         int head_dim, int block_size, kv_dtype dtype, void* stream);
+
+int kvattn_decode_fp8(const void* q, const void* kv_layer, int num_blocks,
+                      const int32_t* block_table, const int32_t* seq_lens, void* out,
+                      int num_seqs, int num_q_heads, int num_kv_heads, int head_dim,
+                      int block_size, int max_blocks_per_seq, int max_seq_len, float scale,
+                      kv_dtype dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+int kvattn_prefill_chunk_fp8(const void* q, const void* kv_layer, int num_blocks,
+                             const int32_t* block_table, const int32_t* seq_lens,
+                             const int32_t* cu_seqlens_q, void* out, int num_seqs,
+                             int total_q_tokens, int max_num_batched_tokens, int num_q_heads,
+                             int num_kv_heads, int head_dim, int block_size,
+                             int max_blocks_per_seq, int max_seq_len, float scale,
+                             kv_dtype dtype, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
+/* ------------------------------------------------------------------------- */
+/* The maps of a step on the GPU, from the requests' lengths: what append, decode and
+ * prefill read, for layers of either format (Section 1: max_num_batched_tokens
+ * bounds the new tokens of one step; Section 2: blocks of fixed size are handed
+ * out as sequences grow).
+ *
+ * cached_lens   device int32 [num_seqs]: tokens in the cache (negative: 0)
+ * new_lens      device int32 [num_seqs]: new tokens a request has (negative: 0)
+ * free_ids      device int32 [num_free]: block ids to hand out, in this order
+ *               (kvblocks_alloc gives such a list)
+ * block_table   device int32 [num_seqs][max_blocks_per_seq], in and out: the first
+ *               ceil(cached / block_size) entries of a row are the blocks it holds
+ * max_tokens    rows of the step (its token budget)
+ * seq_lens      device int32 [num_seqs], out: context with the new tokens
+ * cu_seqlens_q  device int32 [num_seqs + 1], out: request s has rows
+ *               [cu[s], cu[s + 1]) of the step
+ * slot_mapping  device int32 [max_tokens], out: slot of each row's token; -1 for rows
+ *               past cu[num_seqs], and for a token whose block id is negative
+ * positions     device int32 [max_tokens], out: each token's position in its
+ *               sequence; 0 for rows past cu[num_seqs]
+ * used          device int32 [2], out: cu[num_seqs], and the ids the step needs
+ *
+ * A request gets at most what its row of the table has room for, and requests are
+ * served in order until max_tokens are taken: a later one gets fewer of its
+ * new tokens, or none. Request by request the entries that its tokens reach first
+ * take the next free ids; other entries stay. Past the list's end (used[1] >
+ * num_free) entries are -1 and their tokens' slots -1, which append and attention skip.
+ * No output may overlap another argument (KV_ERR_INVALID). At most 65535 requests;
+ * block_size 16. Asynchronous, one launch; allocates nothing; the same
+ * inputs give the same outputs again. */
+int kvattn_step_map(const int32_t* cached_lens, const int32_t* new_lens, int num_seqs,
+                    const int32_t* free_ids, int num_free, int32_t* block_table,
+                    int max_blocks_per_seq, int block_size, int max_tokens, int32_t* seq_lens,
+                    int32_t* cu_seqlens_q, int32_t* slot_mapping, int32_t* positions,
+                    int32_t* used, void* stream);
+
+/* ------------------------------------------------------------------------- */
 /* Elastic per-layer KV pool (Section 3, "Two handles, one virtual range").
  * Each layer owns one reserved virtual range of base + elastic bytes plus one
  * unmapped guard granule. A base physical handle backs [0, base) for the

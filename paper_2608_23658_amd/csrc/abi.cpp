@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "abi_internal.hpp"
+#include "kv_fp8.hpp"
 #include "kvattn.h"
 #include "launch.hpp"
 
@@ -159,7 +160,7 @@ int decode_check(const char* fn, const void* q, const void* kv_layer, const void
                  int num_kv_heads, int head_dim, int block_size, int max_blocks_per_seq,
                  int max_seq_len, float scale, kv_dtype dtype, void* workspace,
                  size_t workspace_bytes, bool check_workspace, void* stream,
-                 kvattn::DecodeArgs* a);
+                 kvattn::DecodeArgs* a, bool fp8 = false);
 
 int decode_launch(const char* fn, const kvattn::DecodeArgs& a);
 
@@ -168,12 +169,12 @@ int decode_common(const char* fn, const void* q, const void* kv_layer, const voi
                   const int32_t* seq_lens, void* out, int num_seqs, int num_q_heads,
                   int num_kv_heads, int head_dim, int block_size, int max_blocks_per_seq,
                   int max_seq_len, float scale, kv_dtype dtype, void* workspace,
-                  size_t workspace_bytes, void* stream) {
+                  size_t workspace_bytes, void* stream, bool fp8 = false) {
   kvattn::DecodeArgs a;
   const int rc = decode_check(fn, q, kv_layer, kv2, num_base, num_blocks, block_table, seq_lens,
                               out, num_seqs, num_q_heads, num_kv_heads, head_dim, block_size,
                               max_blocks_per_seq, max_seq_len, scale, dtype, workspace,
-                              workspace_bytes, true, stream, &a);
+                              workspace_bytes, true, stream, &a, fp8);
   if (rc != KV_OK || num_seqs == 0) return rc;
   return decode_launch(fn, a);
 }
@@ -191,6 +192,26 @@ extern "C" int kvattn_decode(const void* q, const void* kv_layer, int num_blocks
                        seq_lens, out, num_seqs, num_q_heads, num_kv_heads, head_dim,
                        block_size, max_blocks_per_seq, max_seq_len, scale, dtype, workspace,
                        workspace_bytes, stream);
+}
+
+extern "C" size_t kvattn_fp8_block_bytes(int num_kv_heads, int head_dim) {
+  if (num_kv_heads <= 0 || num_kv_heads > 65535 || (head_dim != 64 && head_dim != 128)) return 0;
+  return kvattn::fp8_block_bytes(num_kv_heads, head_dim);
+}
+
+extern "C" int kvattn_decode_fp8(const void* q, const void* kv_layer, int num_blocks,
+                                 const int32_t* block_table, const int32_t* seq_lens, void* out,
+                                 int num_seqs, int num_q_heads, int num_kv_heads, int head_dim,
+                                 int block_size, int max_blocks_per_seq, int max_seq_len,
+                                 float scale, kv_dtype dtype, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  clear_error();
+  if (dtype == KV_F32)
+    return set_error(KV_ERR_UNSUPPORTED, "kvattn_decode_fp8: fp32 queries are not built");
+  return decode_common("kvattn_decode_fp8", q, kv_layer, nullptr, 0, num_blocks, block_table,
+                       seq_lens, out, num_seqs, num_q_heads, num_kv_heads, head_dim,
+                       block_size, max_blocks_per_seq, max_seq_len, scale, dtype, workspace,
+                       workspace_bytes, stream, true);
 }
 
 extern "C" int kvattn_decode_two_tensor(const void* q, const void* kv_base, int num_base_blocks,
@@ -227,7 +248,7 @@ int decode_check(const char* fn, const void* q, const void* kv_layer, const void
                  int num_kv_heads, int head_dim, int block_size, int max_blocks_per_seq,
                  int max_seq_len, float scale, kv_dtype dtype, void* workspace,
                  size_t workspace_bytes, bool check_workspace, void* stream,
-                 kvattn::DecodeArgs* out_args) {
+                 kvattn::DecodeArgs* out_args, bool fp8) {
   if (num_seqs < 0) return set_error(KV_ERR_INVALID, "%s: num_seqs %d < 0", fn, num_seqs);
   if (dtype != KV_F32 && dtype != KV_BF16)
     return set_error(KV_ERR_INVALID, "%s: unknown dtype %d", fn, (int)dtype);
@@ -282,6 +303,7 @@ int decode_check(const char* fn, const void* q, const void* kv_layer, const void
   a.split_tokens = kvattn_decode_split_tokens(max_seq_len);
   a.scale = scale;
   a.bf16 = dtype == KV_BF16;
+  a.fp8 = fp8;
   a.workspace = workspace;
   a.ws_ml_offset = w.ml_offset;
   const size_t room = check_workspace ? std::min(workspace_bytes, kSpreadBytes) : kSpreadBytes;
@@ -315,7 +337,8 @@ extern "C" size_t kvattn_prefill_workspace_bytes(int num_seqs, int total_q_token
   return align256(kvattn::prefill_planned_bytes(num_seqs, total_q_tokens, num_q_heads));
 }
 
-extern "C" int kvattn_prefill_chunk(const void* q, const void* kv_layer, int num_blocks,
+namespace {
+int prefill_common(const char* fn, bool fp8, const void* q, const void* kv_layer, int num_blocks,
                                     const int32_t* block_table, const int32_t* seq_lens,
                                     const int32_t* cu_seqlens_q, void* out, int num_seqs,
                                     int total_q_tokens, int max_num_batched_tokens,
@@ -323,48 +346,50 @@ extern "C" int kvattn_prefill_chunk(const void* q, const void* kv_layer, int num
                                     int block_size, int max_blocks_per_seq, int max_seq_len,
                                     float scale, kv_dtype dtype, void* workspace,
                                     size_t workspace_bytes, void* stream) {
-  clear_error();
   if (dtype == KV_F32)
-    return set_error(KV_ERR_UNSUPPORTED, "kvattn_prefill_chunk: fp32 prefill is not built");
+    return set_error(KV_ERR_UNSUPPORTED, "%s: fp32 prefill is not built", fn);
   if (dtype != KV_BF16)
-    return set_error(KV_ERR_INVALID, "kvattn_prefill_chunk: unknown dtype %d", (int)dtype);
+    return set_error(KV_ERR_INVALID, "%s: unknown dtype %d", fn, (int)dtype);
   if (num_seqs < 0 || total_q_tokens < 0)
-    return set_error(KV_ERR_INVALID, "kvattn_prefill_chunk: negative sizes");
+    return set_error(KV_ERR_INVALID, "%s: negative sizes", fn);
   if (total_q_tokens > max_num_batched_tokens)
     return set_error(KV_ERR_INVALID,
-                     "kvattn_prefill_chunk: %d new tokens exceed max_num_batched_tokens %d",
+                     "%s: %d new tokens exceed max_num_batched_tokens %d", fn,
                      total_q_tokens, max_num_batched_tokens);
   if (num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads)
-    return set_error(KV_ERR_INVALID, "kvattn_prefill_chunk: %d query heads over %d kv heads",
+    return set_error(KV_ERR_INVALID, "%s: %d query heads over %d kv heads", fn,
                      num_q_heads, num_kv_heads);
   if (!group_ok(num_q_heads, num_kv_heads, 8))
-    return set_error(KV_ERR_UNSUPPORTED, "kvattn_prefill_chunk: group size %d not built",
+    return set_error(KV_ERR_UNSUPPORTED, "%s: group size %d not built", fn,
                      num_q_heads / num_kv_heads);
   if (head_dim != 128)
-    return set_error(KV_ERR_UNSUPPORTED, "kvattn_prefill_chunk: head_dim %d not built",
+    return set_error(KV_ERR_UNSUPPORTED, "%s: head_dim %d not built", fn,
                      head_dim);
   if (block_size != 16)
-    return set_error(KV_ERR_UNSUPPORTED, "kvattn_prefill_chunk: block_size %d not built",
+    return set_error(KV_ERR_UNSUPPORTED, "%s: block_size %d not built", fn,
                      block_size);
   if (max_blocks_per_seq <= 0 || max_seq_len < 0 ||
       (long long)max_seq_len > (long long)max_blocks_per_seq * block_size)
     return set_error(KV_ERR_INVALID,
-                     "kvattn_prefill_chunk: max_seq_len %d does not fit %d blocks of %d tokens",
+                     "%s: max_seq_len %d does not fit %d blocks of %d tokens", fn,
                      max_seq_len, max_blocks_per_seq, block_size);
   if (num_blocks <= 0)
-    return set_error(KV_ERR_INVALID, "kvattn_prefill_chunk: num_blocks %d", num_blocks);
+    return set_error(KV_ERR_INVALID, "%s: num_blocks %d", fn, num_blocks);
   if (!std::isfinite(scale))
-    return set_error(KV_ERR_INVALID, "kvattn_prefill_chunk: scale not finite");
-  if (num_kv_heads > 65535) return set_error(KV_ERR_UNSUPPORTED, "kvattn_prefill_chunk: grid");
+    return set_error(KV_ERR_INVALID, "%s: scale not finite", fn);
+  // masked scores are minus infinity before the scale
+  if (fp8 && !(scale > 0.f))
+    return set_error(KV_ERR_INVALID, "%s: scale %g must be above zero", fn, scale);
+  if (num_kv_heads > 65535) return set_error(KV_ERR_UNSUPPORTED, "%s: grid", fn);
   if (num_seqs == 0 || total_q_tokens == 0) return KV_OK;
   if (!q || !kv_layer || !block_table || !seq_lens || !cu_seqlens_q || !out || !workspace)
-    return set_error(KV_ERR_INVALID, "kvattn_prefill_chunk: null pointer argument");
+    return set_error(KV_ERR_INVALID, "%s: null pointer argument", fn);
   if (!aligned16(q) || !aligned16(kv_layer) || !aligned16(out) || !aligned16(workspace))
-    return set_error(KV_ERR_INVALID, "kvattn_prefill_chunk: q, kv_layer, out and workspace "
-                                     "must be 16-byte aligned");
+    return set_error(KV_ERR_INVALID, "%s: q, kv_layer, out and workspace "
+                                     "must be 16-byte aligned", fn);
   const size_t need = prefill_min_bytes(num_seqs, total_q_tokens);
   if (workspace_bytes < need)
-    return set_error(KV_ERR_INVALID, "kvattn_prefill_chunk: workspace %zu bytes < %zu needed",
+    return set_error(KV_ERR_INVALID, "%s: workspace %zu bytes < %zu needed", fn,
                      workspace_bytes, need);
   kvattn::PrefillArgs a;
   a.q = q;
@@ -382,13 +407,45 @@ extern "C" int kvattn_prefill_chunk(const void* q, const void* kv_layer, int num
   a.max_blocks = max_blocks_per_seq;
   a.max_seq_len = max_seq_len;
   a.scale = scale;
+  a.fp8 = fp8;
   a.workspace = workspace;
   a.workspace_bytes = workspace_bytes;
   a.stream = static_cast<hipStream_t>(stream);
   const hipError_t e = kvattn::launch_prefill(a);
   if (e == hipErrorNotSupported)
-    return set_error(KV_ERR_UNSUPPORTED, "kvattn_prefill_chunk: kernel not built");
-  return hip_status(e, "kvattn_prefill_chunk launch");
+    return set_error(KV_ERR_UNSUPPORTED, "%s: kernel not built", fn);
+  return hip_status(e, fn);
+}
+}  // namespace
+
+extern "C" int kvattn_prefill_chunk(const void* q, const void* kv_layer, int num_blocks,
+                                    const int32_t* block_table, const int32_t* seq_lens,
+                                    const int32_t* cu_seqlens_q, void* out, int num_seqs,
+                                    int total_q_tokens, int max_num_batched_tokens,
+                                    int num_q_heads, int num_kv_heads, int head_dim,
+                                    int block_size, int max_blocks_per_seq, int max_seq_len,
+                                    float scale, kv_dtype dtype, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+  clear_error();
+  return prefill_common("kvattn_prefill_chunk", false, q, kv_layer, num_blocks, block_table, seq_lens,
+                        cu_seqlens_q, out, num_seqs, total_q_tokens, max_num_batched_tokens,
+                        num_q_heads, num_kv_heads, head_dim, block_size, max_blocks_per_seq,
+                        max_seq_len, scale, dtype, workspace, workspace_bytes, stream);
+}
+
+extern "C" int kvattn_prefill_chunk_fp8(const void* q, const void* kv_layer, int num_blocks,
+                                    const int32_t* block_table, const int32_t* seq_lens,
+                                    const int32_t* cu_seqlens_q, void* out, int num_seqs,
+                                    int total_q_tokens, int max_num_batched_tokens,
+                                    int num_q_heads, int num_kv_heads, int head_dim,
+                                    int block_size, int max_blocks_per_seq, int max_seq_len,
+                                    float scale, kv_dtype dtype, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+  clear_error();
+  return prefill_common("kvattn_prefill_chunk_fp8", true, q, kv_layer, num_blocks, block_table, seq_lens,
+                        cu_seqlens_q, out, num_seqs, total_q_tokens, max_num_batched_tokens,
+                        num_q_heads, num_kv_heads, head_dim, block_size, max_blocks_per_seq,
+                        max_seq_len, scale, dtype, workspace, workspace_bytes, stream);
 }
 
 extern "C" int kvattn_kv_append(const void* k_new, const void* v_new,
@@ -435,6 +492,104 @@ extern "C" int kvattn_kv_append(const void* k_new, const void* v_new,
     return set_error(KV_ERR_UNSUPPORTED,
                      "kvattn_kv_append: rows must be 64 to 512 bytes in steps of 64");
   return hip_status(e, "kvattn_kv_append launch");
+}
+
+extern "C" int kvattn_kv_append_fp8(const void* k_new, const void* v_new,
+                                    const int32_t* slot_mapping, void* kv_layer, int num_blocks,
+                                    int num_tokens, int num_kv_heads, int head_dim,
+                                    int block_size, kv_dtype dtype, void* stream) {
+  clear_error();
+  const char* fn = "kvattn_kv_append_fp8";
+  if (dtype != KV_F32 && dtype != KV_BF16)
+    return set_error(KV_ERR_INVALID, "%s: unknown dtype %d", fn, (int)dtype);
+  if (num_tokens < 0) return set_error(KV_ERR_INVALID, "%s: num_tokens < 0", fn);
+  if (num_kv_heads <= 0 || head_dim <= 0)
+    return set_error(KV_ERR_INVALID, "%s: %d kv heads of dim %d", fn, num_kv_heads, head_dim);
+  if (num_kv_heads > 65535) return set_error(KV_ERR_UNSUPPORTED, "%s: grid too large", fn);
+  if (head_dim != 64 && head_dim != 128)
+    return set_error(KV_ERR_UNSUPPORTED, "%s: head_dim %d not built", fn, head_dim);
+  if (block_size != 16)
+    return set_error(KV_ERR_UNSUPPORTED, "%s: block_size %d not built", fn, block_size);
+  if (num_blocks <= 0 || (long long)num_blocks * block_size > 0x7fffffffLL)
+    return set_error(KV_ERR_INVALID, "%s: num_blocks %d", fn, num_blocks);
+  if (num_tokens == 0) return KV_OK;
+  if (!k_new || !v_new || !slot_mapping || !kv_layer)
+    return set_error(KV_ERR_INVALID, "%s: null pointer argument", fn);
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(kv_layer))
+    return set_error(KV_ERR_INVALID, "%s: k_new, v_new and kv_layer must be 16-byte aligned", fn);
+  kvattn::AppendArgs a;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.slot_mapping = slot_mapping;
+  a.kv = kv_layer;
+  a.num_blocks = num_blocks;
+  a.num_tokens = num_tokens;
+  a.num_kv_heads = num_kv_heads;
+  a.head_dim = head_dim;
+  a.esz = dtype == KV_BF16 ? 2 : 4;
+  a.stream = static_cast<hipStream_t>(stream);
+  return hip_status(kvattn::launch_append_fp8(a), fn);
+}
+
+namespace {
+struct Range {
+  const void* p;
+  size_t bytes;
+};
+bool overlap(const Range& a, const Range& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+}
+}  // namespace
+
+extern "C" int kvattn_step_map(const int32_t* cached_lens, const int32_t* new_lens, int num_seqs,
+                               const int32_t* free_ids, int num_free, int32_t* block_table,
+                               int max_blocks_per_seq, int block_size, int max_tokens,
+                               int32_t* seq_lens, int32_t* cu_seqlens_q, int32_t* slot_mapping,
+                               int32_t* positions, int32_t* used, void* stream) {
+  clear_error();
+  const char* fn = "kvattn_step_map";
+  if (num_seqs < 0 || num_free < 0 || max_tokens < 0)
+    return set_error(KV_ERR_INVALID, "%s: negative sizes", fn);
+  if (num_seqs > 65535) return set_error(KV_ERR_UNSUPPORTED, "%s: %d sequences", fn, num_seqs);
+  if (block_size != 16)
+    return set_error(KV_ERR_UNSUPPORTED, "%s: block_size %d not built", fn, block_size);
+  if (max_blocks_per_seq <= 0 || (long long)max_blocks_per_seq * block_size > 0x7fffffffLL)
+    return set_error(KV_ERR_INVALID, "%s: %d blocks per sequence", fn, max_blocks_per_seq);
+  const Range ranges[] = {   // the first kWritten are written
+      {block_table, (size_t)num_seqs * max_blocks_per_seq * 4},
+      {seq_lens, (size_t)num_seqs * 4},
+      {cu_seqlens_q, ((size_t)num_seqs + 1) * 4},
+      {slot_mapping, (size_t)max_tokens * 4},
+      {positions, (size_t)max_tokens * 4},
+      {used, 2 * 4},
+      {cached_lens, (size_t)num_seqs * 4},
+      {new_lens, (size_t)num_seqs * 4},
+      {free_ids, (size_t)num_free * 4}};
+  constexpr int kRanges = sizeof(ranges) / sizeof(ranges[0]), kWritten = 6;
+  for (const Range& r : ranges)
+    if (r.bytes && (!r.p || (reinterpret_cast<uintptr_t>(r.p) & 3)))
+      return set_error(KV_ERR_INVALID, "%s: null or not 4-byte aligned argument", fn);
+  for (int i = 0; i < kWritten; ++i)
+    for (int j = i + 1; j < kRanges; ++j)
+      if (overlap(ranges[i], ranges[j]))
+        return set_error(KV_ERR_INVALID, "%s: an output overlaps another argument", fn);
+  kvattn::StepMapArgs a;
+  a.cached = cached_lens;
+  a.wanted = new_lens;
+  a.num_seqs = num_seqs;
+  a.free_ids = free_ids;
+  a.num_free = num_free;
+  a.block_table = block_table;
+  a.max_blocks = max_blocks_per_seq;
+  a.max_tokens = max_tokens;
+  a.seq_lens = seq_lens;
+  a.cu_seqlens_q = cu_seqlens_q;
+  a.slot_mapping = slot_mapping;
+  a.positions = positions;
+  a.used = used;
+  a.stream = static_cast<hipStream_t>(stream);
+  return hip_status(kvattn::launch_step_map(a), fn);
 }
 
 extern "C" int kvattn_copy_blocks(void* const* layers, int num_layers, int num_blocks,

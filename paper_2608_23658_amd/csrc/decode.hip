@@ -100,6 +100,7 @@
 
 #include "common.hpp"
 #include "decode_walk.hpp"
+#include "kv_fp8.hpp"
 #include "launch.hpp"
 
 namespace kvattn {
@@ -297,8 +298,8 @@ __device__ __forceinline__ int share_tokens(int n) {
 // kSpread: one wavefront's share is a workgroup of its own. kAhead: the walk
 // loads a step ahead. kTurns: a workgroup of fewer wavefronts than shares, which
 // take turns, and with a piece of the context instead of one split. None of
-// them changes a result.
-template <int D, int G, bool BF16, bool kTwo, bool kAhead, bool kSpread, bool kTurns>
+// them changes a result. kFp8: the cache is in 8 bits (q and out in bf16).
+template <int D, int G, bool BF16, bool kTwo, bool kAhead, bool kSpread, bool kTurns, bool kFp8>
 __global__ __attribute__((amdgpu_flat_work_group_size(kWave, kDecodeWaves * kWave),
                           amdgpu_waves_per_eu(kAhead && D == 128 ? 1 : 2)))
 void decode_split_kernel(
@@ -336,6 +337,7 @@ void decode_split_kernel(
   const size_t head_off = (size_t)g * tile_bytes;
   const DecodeTiles<kTwo> tiles = {kv, kv2, num_base, 2 * (size_t)num_kv_heads * tile_bytes,
                                    head_off, (size_t)num_kv_heads * tile_bytes + head_off};
+  const Fp8Tiles tiles8(kv, num_kv_heads, D, g);   // kFp8
   const uint8_t* q_row = q + ((size_t)s * num_q_heads + h0) * row_bytes;
 
   constexpr int kStates = kSpread ? 1 : W;
@@ -354,9 +356,13 @@ void decode_split_kernel(
     if constexpr (kSpread) {   // one share: its state goes out as it is
       if (wave >= parts) return;
       const int t0 = s0 + wave * part_tokens;
-      walk_bf16<D, G, kTwo, kAhead>(tiles, reinterpret_cast<const uint16_t*>(q_row), bt,
-                                    num_blocks, t0, min(s1, t0 + part_tokens), scale_log2,
-                                    o_lds[0], ml_lds[0]);
+      if constexpr (kFp8)
+        walk_fp8<D, G, kAhead>(tiles8, reinterpret_cast<const uint16_t*>(q_row), bt, num_blocks,
+                               t0, min(s1, t0 + part_tokens), scale_log2, o_lds[0], ml_lds[0]);
+      else
+        walk_bf16<D, G, kTwo, kAhead>(tiles, reinterpret_cast<const uint16_t*>(q_row), bt,
+                                      num_blocks, t0, min(s1, t0 + part_tokens), scale_log2,
+                                      o_lds[0], ml_lds[0]);
       wave_lds_sync();
       const size_t row = (size_t)s * num_q_heads + h0;
       for (int e = threadIdx.x; e < G * D / 4; e += kWave) {
@@ -383,9 +389,13 @@ void decode_split_kernel(
     if constexpr (BF16) {
       for (int p = wave; p < parts; p += step) {
         const int t0 = s0 + p * part_tokens;
-        walk_bf16<D, G, kTwo, kAhead>(tiles, reinterpret_cast<const uint16_t*>(q_row), bt,
-                                      num_blocks, t0, min(s1, t0 + part_tokens), scale_log2,
-                                      o_lds[p], ml_lds[p]);
+        if constexpr (kFp8)
+          walk_fp8<D, G, kAhead>(tiles8, reinterpret_cast<const uint16_t*>(q_row), bt, num_blocks,
+                                 t0, min(s1, t0 + part_tokens), scale_log2, o_lds[p], ml_lds[p]);
+        else
+          walk_bf16<D, G, kTwo, kAhead>(tiles, reinterpret_cast<const uint16_t*>(q_row), bt,
+                                        num_blocks, t0, min(s1, t0 + part_tokens), scale_log2,
+                                        o_lds[p], ml_lds[p]);
         if constexpr (!kTurns) break;
       }
     } else {
@@ -592,7 +602,7 @@ __global__ __launch_bounds__(kCombineWaves * kWave) void decode_combine_kernel(
   write_row4<BF16>(out, (size_t)w * kLPS + col, l, make_float4(o[0], o[1], o[2], o[3]));
 }
 
-template <int D, int G, bool BF16, bool kTwo = false>
+template <int D, int G, bool BF16, bool kTwo = false, bool kFp8 = false>
 static hipError_t launch_decode_t(const DecodeArgs& a) {
   const int max_splits = (a.max_seq_len + a.split_tokens - 1) / a.split_tokens;
   const int splits = max_splits > 0 ? max_splits : 1;
@@ -617,16 +627,17 @@ static hipError_t launch_decode_t(const DecodeArgs& a) {
     const long long pieces = std::max(kMinPieces, kMostBlocks / per_piece);
     blocks = per_piece * std::min<long long>(splits, pieces);
   }
-  auto split = decode_split_kernel<D, G, BF16, kTwo, false, false, false>;
-  if (turns) split = decode_split_kernel<D, G, BF16, kTwo, false, false, true>;
+  auto split = decode_split_kernel<D, G, BF16, kTwo, false, false, false, kFp8>;
+  if (turns) split = decode_split_kernel<D, G, BF16, kTwo, false, false, true, kFp8>;
   if constexpr (kCanSpread) {
     if (spread)
-      split = decode_split_kernel<D, G, BF16, kTwo, true, true, false>;
+      split = decode_split_kernel<D, G, BF16, kTwo, true, true, false, kFp8>;
     else if constexpr (D == 64)
       if (max_splits > 1 && !turns && blocks <= kAheadBlocks)
-        split = decode_split_kernel<D, G, BF16, kTwo, true, false, false>;
+        split = decode_split_kernel<D, G, BF16, kTwo, true, false, false, kFp8>;
   }
-  trace_before(a.stream, kTwo ? "decode_split_two_tensor" : "decode_split");
+  trace_before(a.stream, kTwo ? "decode_split_two_tensor"
+                         : kFp8 ? "decode_split_fp8" : "decode_split");
   hipLaunchKernelGGL(split, dim3((unsigned)(spread ? blocks * kDecodeWaves : blocks)),
                      dim3(waves * kWave), 0, a.stream, static_cast<const uint8_t*>(a.q),
                      static_cast<const uint8_t*>(a.kv), static_cast<const uint8_t*>(a.kv2),
@@ -656,13 +667,13 @@ static hipError_t launch_decode_t(const DecodeArgs& a) {
   return hipGetLastError();
 }
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool kFp8 = false>
 static hipError_t dispatch_g(const DecodeArgs& a, int G) {
   switch (G) {
-    case 1: return launch_decode_t<D, 1, BF16>(a);
-    case 2: return launch_decode_t<D, 2, BF16>(a);
-    case 4: return launch_decode_t<D, 4, BF16>(a);
-    case 8: return launch_decode_t<D, 8, BF16>(a);
+    case 1: return launch_decode_t<D, 1, BF16, false, kFp8>(a);
+    case 2: return launch_decode_t<D, 2, BF16, false, kFp8>(a);
+    case 4: return launch_decode_t<D, 4, BF16, false, kFp8>(a);
+    case 8: return launch_decode_t<D, 8, BF16, false, kFp8>(a);
     default: return hipErrorInvalidValue;
   }
 }
@@ -679,7 +690,10 @@ hipError_t launch_decode(const DecodeArgs& a) {
       default: return hipErrorInvalidValue;
     }
   }
-  if (a.bf16) {
+  if (a.fp8) {
+    if (a.head_dim == 128) return dispatch_g<128, true, true>(a, G);
+    if (a.head_dim == 64) return dispatch_g<64, true, true>(a, G);
+  } else if (a.bf16) {
     if (a.head_dim == 128) return dispatch_g<128, true>(a, G);
     if (a.head_dim == 64) return dispatch_g<64, true>(a, G);
   } else {

@@ -11,7 +11,7 @@ import ctypes
 import math
 import os
 import re
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -77,6 +77,13 @@ def lib() -> ctypes.CDLL:
     _c(L.kvattn_prefill_chunk, i32, vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32,
        i32, i32, i32, f32, i32, vp, sz, vp)
     _c(L.kvattn_kv_append, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp)
+    _c(L.kvattn_fp8_block_bytes, sz, i32, i32)
+    _c(L.kvattn_kv_append_fp8, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp)
+    _c(L.kvattn_decode_fp8, i32, vp, vp, i32, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, f32,
+       i32, vp, sz, vp)
+    _c(L.kvattn_prefill_chunk_fp8, i32, vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32,
+       i32, i32, i32, f32, i32, vp, sz, vp)
+    _c(L.kvattn_step_map, i32, vp, vp, i32, vp, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp)
     _c(L.kvpool_granularity, i32, i32, ctypes.POINTER(ctypes.c_size_t))
     _c(L.kvpool_create, i32, i32, i32, sz, sz, ctypes.POINTER(vp))
     _c(L.kvpool_layer_ptr, i32, vp, i32, ctypes.POINTER(vp))
@@ -358,6 +365,166 @@ def kv_append(k_new: torch.Tensor, v_new: torch.Tensor, slot_mapping: torch.Tens
                                 _ptr(kv_layer), int(num_blocks), T, Hkv, d, int(block_size),
                                 _dtype_code(k_new.dtype), _stream(stream))
     check(rc)
+
+
+def _require_current_device(*ts):
+    """Launches go to the current device: tensors of another one are refused."""
+    cur = torch.cuda.current_device()
+    for t in ts:
+        if isinstance(t, torch.Tensor) and t.device.index != cur:
+            raise ValueError(f"tensors must be on the current device (cuda:{cur}), "
+                             f"not {t.device}")
+
+
+def _for_stream(stream, *ts):
+    """Tensors made here that a call uses on a stream of the caller's choice: the
+    allocator must not hand them out again before that stream is done."""
+    if stream is None:
+        return
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    for t in ts:
+        t.record_stream(stream)
+
+
+def fp8_block_bytes(num_kv_heads: int, head_dim: int) -> int:
+    """Bytes of one block of a layer in 8 bits (also copy_blocks' block_bytes)."""
+    return int(lib().kvattn_fp8_block_bytes(num_kv_heads, head_dim))
+
+
+def _require_fp8_layer(kv_layer, num_blocks: int, num_kv_heads: int, head_dim: int):
+    if isinstance(kv_layer, torch.Tensor):
+        have = kv_layer.numel() * kv_layer.element_size()
+        need = int(num_blocks) * fp8_block_bytes(num_kv_heads, head_dim)
+        if have < need:
+            raise ValueError(f"kv_layer has {have} bytes, {num_blocks} blocks need {need}")
+
+
+def kv_append_fp8(k_new: torch.Tensor, v_new: torch.Tensor, slot_mapping: torch.Tensor, kv_layer,
+                  num_blocks: int, *, block_size: int = 16, stream=None) -> None:
+    """Write ``k_new``/``v_new`` [T, Hkv, d] (bf16 or fp32) into the slots ``slot_mapping``
+    [T] int32 of a layer in 8 bits; tokens of one block must stand together."""
+    T, Hkv, d = k_new.shape
+    if v_new.shape != k_new.shape or v_new.dtype != k_new.dtype:
+        raise ValueError("k_new and v_new must have the same shape and dtype")
+    if slot_mapping.dtype != torch.int32 or tuple(slot_mapping.shape) != (T,):
+        raise ValueError("slot_mapping must be int32 [num_tokens]")
+    code = _dtype_code(k_new.dtype)
+    _require_fp8_layer(kv_layer, num_blocks, Hkv, d)
+    _require_cuda(k_new, v_new, slot_mapping, kv_layer)
+    _require_current_device(k_new, v_new, slot_mapping, kv_layer)
+    check(lib().kvattn_kv_append_fp8(k_new.data_ptr(), v_new.data_ptr(), slot_mapping.data_ptr(),
+                                     _ptr(kv_layer), int(num_blocks), T, Hkv, d, int(block_size),
+                                     code, _stream(stream)))
+
+
+def decode_fp8(q: torch.Tensor, kv_layer, num_blocks: int, block_table: torch.Tensor,
+               seq_lens: torch.Tensor, *, num_kv_heads: int, max_seq_len: int,
+               block_size: int = 16, scale: Optional[float] = None,
+               out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """``decode`` over a layer in 8 bits: ``q`` [B, Hq, d] bf16 -> out [B, Hq, d]."""
+    B, Hq, d = q.shape
+    _require_batch(B, block_table, seq_lens)
+    _require_out(out, q)
+    code = _dtype_code(q.dtype)
+    _require_fp8_layer(kv_layer, num_blocks, num_kv_heads, d)
+    _require_cuda(q, kv_layer, block_table, seq_lens, out, ws)
+    _require_current_device(q, kv_layer, block_table, seq_lens, out, ws)
+    if out is None:
+        out = torch.empty_like(q)
+        _for_stream(stream, out)
+    if ws is None:
+        ws = workspace(decode_workspace_bytes(B, Hq, d, max_seq_len), q.device)
+        _for_stream(stream, ws)
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    check(lib().kvattn_decode_fp8(q.data_ptr(), _ptr(kv_layer), int(num_blocks),
+                                  block_table.data_ptr(), seq_lens.data_ptr(), out.data_ptr(), B,
+                                  Hq, int(num_kv_heads), d, int(block_size),
+                                  int(block_table.shape[1]), int(max_seq_len), float(scale), code,
+                                  ws.data_ptr(), ws.numel(), _stream(stream)))
+    return out
+
+
+def prefill_chunk_fp8(q: torch.Tensor, kv_layer, num_blocks: int, block_table: torch.Tensor,
+                      seq_lens: torch.Tensor, cu_seqlens_q: torch.Tensor, *, num_kv_heads: int,
+                      max_seq_len: int, max_num_batched_tokens: Optional[int] = None,
+                      block_size: int = 16, scale: Optional[float] = None,
+                      out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                      stream=None) -> torch.Tensor:
+    """``prefill_chunk`` over a layer in 8 bits: ``q`` [T, Hq, d] bf16."""
+    T, Hq, d = q.shape
+    _require_int32(block_table=block_table, seq_lens=seq_lens, cu_seqlens_q=cu_seqlens_q)
+    B = int(seq_lens.shape[0])
+    _require_rows(B, block_table, seq_lens, cu_seqlens_q)
+    _require_out(out, q)
+    code = _dtype_code(q.dtype)
+    _require_fp8_layer(kv_layer, num_blocks, num_kv_heads, d)
+    _require_cuda(q, kv_layer, block_table, seq_lens, cu_seqlens_q, out, ws)
+    _require_current_device(q, kv_layer, block_table, seq_lens, cu_seqlens_q, out, ws)
+    if out is None:
+        out = torch.empty_like(q)
+        _for_stream(stream, out)
+    if ws is None:
+        ws = workspace(prefill_workspace_bytes(B, T, Hq, d), q.device)
+        _for_stream(stream, ws)
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    budget = T if max_num_batched_tokens is None else int(max_num_batched_tokens)
+    check(lib().kvattn_prefill_chunk_fp8(q.data_ptr(), _ptr(kv_layer), int(num_blocks),
+                                         block_table.data_ptr(), seq_lens.data_ptr(),
+                                         cu_seqlens_q.data_ptr(), out.data_ptr(), B, T, budget, Hq,
+                                         int(num_kv_heads), d, int(block_size),
+                                         int(block_table.shape[1]), int(max_seq_len),
+                                         float(scale), code, ws.data_ptr(), ws.numel(),
+                                         _stream(stream)))
+    return out
+
+
+class StepMap(NamedTuple):
+    """What ``step_map`` writes beside the block table, all int32 on the GPU."""
+    seq_lens: torch.Tensor        # [num_seqs]
+    cu_seqlens_q: torch.Tensor    # [num_seqs + 1]
+    slot_mapping: torch.Tensor    # [max_tokens]
+    positions: torch.Tensor       # [max_tokens]
+    used: torch.Tensor            # [2]: new tokens taken, block ids needed
+
+    @staticmethod
+    def empty(num_seqs: int, max_tokens: int, device=None) -> "StepMap":
+        """Room for the maps of a step, to be kept and passed as ``out``."""
+        sizes = [num_seqs, num_seqs + 1, max_tokens, max_tokens, 2]
+        return StepMap(*torch.empty(sum(sizes), dtype=torch.int32,
+                                    device=device if device is not None else "cuda").split(sizes))
+
+
+def step_map(cached_lens: torch.Tensor, new_lens: torch.Tensor, free_ids: torch.Tensor,
+             block_table: torch.Tensor, *, max_tokens: int, block_size: int = 16,
+             out: Optional[StepMap] = None, stream=None) -> StepMap:
+    """The maps of a step from the requests' lengths (``cached_lens`` and ``new_lens``
+    [num_seqs] int32); new entries of ``block_table`` [num_seqs, max_blocks] take the ids of
+    ``free_ids`` in order. ``out.used[1]`` counts the ids taken."""
+    S = int(cached_lens.shape[0])
+    _require_int32(cached_lens=cached_lens, new_lens=new_lens, free_ids=free_ids,
+                   block_table=block_table)
+    if cached_lens.dim() != 1 or new_lens.shape != cached_lens.shape or free_ids.dim() != 1:
+        raise ValueError("cached_lens and new_lens must be [num_seqs], free_ids one-dimensional")
+    if block_table.shape[0] != S:
+        raise ValueError(f"block_table must have {S} rows, not {block_table.shape[0]}")
+    if out is not None:
+        want = (S, S + 1, max_tokens, max_tokens, 2)
+        if any(t.dtype != torch.int32 or tuple(t.shape) != (n,) for t, n in zip(out, want)):
+            raise ValueError("out must be int32 tensors as StepMap.empty(num_seqs, max_tokens)")
+    _require_cuda(cached_lens, new_lens, free_ids, block_table, *(out or ()))
+    _require_current_device(cached_lens, new_lens, free_ids, block_table, *(out or ()))
+    if out is None:
+        out = StepMap.empty(S, max_tokens, block_table.device)
+        _for_stream(stream, *out)
+    check(lib().kvattn_step_map(cached_lens.data_ptr(), new_lens.data_ptr(), S,
+                                free_ids.data_ptr(), int(free_ids.numel()),
+                                block_table.data_ptr(), int(block_table.shape[1]),
+                                int(block_size), int(max_tokens), out.seq_lens.data_ptr(),
+                                out.cu_seqlens_q.data_ptr(), out.slot_mapping.data_ptr(),
+                                out.positions.data_ptr(), out.used.data_ptr(), _stream(stream)))
+    return out
 
 
 class KernelTrace:
