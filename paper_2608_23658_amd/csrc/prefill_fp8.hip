@@ -1,16 +1,23 @@
 // Chunked-prefill attention over a cache in 8 bits: the tiles, plan, partials and
 // merge of the bf16 prefill, with a tile pipeline that converts what it gathers.
 //
-// A step's K and V (64 keys) are gathered as they lie, 8 KiB each, straight into a
-// raw LDS buffer; each wavefront then reads back the 1 KiB of K and of V that it
-// gathered itself (so it waits for its own loads alone, no barrier), converts
-// them to bf16 times their block's power of two, exactly, and writes them into the LDS
-// tiles that the products read, in the order the bf16 tiles have. Sixteen
-// conversions a thread and step serve all eight wavefronts; converting on the
-// way from LDS to the matrix unit instead would take each wavefront 128. The
-// products, the softmax and its lazy reference, the partials and the output are
-// those of the bf16 tile, and so is what bounds a step: the matrix unit and,
-// beside it, LDS reads (256 KiB for 1 MiFLOP of each of 8 wavefronts).
+// A step's K and V (64 keys) are 8 KiB each: 16 bytes a thread. Each thread loads its
+// piece into registers one step ahead, converts it to bf16 times its block's power of
+// two, exactly, and writes it into the LDS tiles that the products read, in the order
+// the bf16 tiles have. Sixteen conversions a thread and step serve all eight
+// wavefronts; converting on the way from LDS to the matrix unit instead would take
+// each wavefront 128, beside a vector unit that the softmax fills. The products, the
+// softmax and its lazy reference, the partials and the output are those of the bf16
+// tile, and so is what bounds a step: the matrix unit, the vector unit and LDS reads
+// (256 KiB for 1 MiFLOP of each of 8 wavefronts) in nearly equal parts.
+//
+// 8192 rows over 24576 cached tokens, 32 query heads over 8, on one box after
+// another (the bf16 kernel takes 3.27 to 3.32 ms):
+//   gathered into raw LDS buffers, read back, converted and written     3.88 ms
+//   buffers' addresses as constants, one address for a lane's writes     0.93 of that
+//   no branch among the issue slots, the last step in one form           0.88
+//   through registers instead of LDS, addresses held, no raised priority 0.86
+// (The branch had made the compiler sink half of a step's exponentials behind it.)
 //
 // Slots that must not contribute (past the sequence's end, or of a block id
 // outside the layer) are zeroed in V as they are converted and masked in the scores.
@@ -25,7 +32,6 @@
 namespace kvattn {
 
 namespace {
-constexpr int kRawTile = kBS * kD;       // one (block, K/V, head) tile in e4m3: 2 KiB
 constexpr int kTile = kBS * kD * 2;      // the same in bf16
 constexpr int kBufs = 2;                 // LDS steps of each kind
 
@@ -55,8 +61,8 @@ __device__ __forceinline__ void prefill_tile_fp8(
   const bool idle = row0 >= n;                  // none of the wave's 32 rows is in the chunk
 
   struct Lds {
-    uint8_t raw[kBufs][2][kStepBlocks][kRawTile];   // K, V as gathered
-    uint8_t k[kBufs][kStepBlocks][kTile], v[kBufs][kStepBlocks][kTile];
+    uint8_t v[kBufs][kStepBlocks][kTile], k[kBufs][kStepBlocks][kTile];
+    uint8_t more[kWaves * 32 * 144 - kBufs * kStepBlocks * kTile];   // the rows of the end
     // what only the end needs, kept off the scalar registers of the loop
     struct {
       uint16_t* out;    // of this kv head's first query head, row 0
@@ -102,7 +108,7 @@ __device__ __forceinline__ void prefill_tile_fp8(
   float m_ref = -INFINITY;   // reference max of the lane's row (log2 domain)
   float l_run = 0.f;         // lane-partial row sum
 
-  // ---- gather of a step straight into the raw buffers (global_load_lds) ----
+  // ---- gather of a step into registers ----
   // The block ids of a step are read from the table first (step_ids), in
   // SGPRs: one 16-byte scalar load when all 4 blocks lie inside the sequence,
   // single entries otherwise; a block past L or with an id outside
@@ -146,18 +152,11 @@ __device__ __forceinline__ void prefill_tile_fp8(
   };
   auto real = [&](int id) __attribute__((always_inline)) { return real_id(id) ? id : -1; };
   auto my_block = [&](int id) __attribute__((always_inline)) { return tiles.block(max(id, 0)); };
-  // One gather of K (kind 0) or V (1) per wavefront into raw buffer `buf`, two at a time.
-  auto gather2 = [&](int id_a, int kind_a, int buf_a, int id_b, int kind_b,
-                     int buf_b) __attribute__((always_inline)) {
-    // the lane id is recomputed here rather than kept live across the step
-    const uint32_t off = my_half * 1024 + lane_id_fresh() * 16;
-    const uint32_t mine =   // tiles of 2 KiB in block order: wavefront w's part is KiB w
-        __builtin_amdgcn_readfirstlane(lds_addr(&lds.raw[0][0][0][0]) + wave * 1024);
-    dma16x2(my_block(id_a) + (kind_a ? tiles.v_off : tiles.k_off), off,
-            mine + (buf_a * 2 + kind_a) * (kStepBlocks * kRawTile),
-            my_block(id_b) + (kind_b ? tiles.v_off : tiles.k_off), off,
-            mine + (buf_b * 2 + kind_b) * (kStepBlocks * kRawTile));
+  // This lane's 16 bytes of the K or V tile (at part) of a block.
+  auto gather = [&](int id, uint32_t part) __attribute__((always_inline)) {
+    return *reinterpret_cast<const uint4*>(my_block(id) + (part + my_half * 1024) + (uint32_t)lane * 16);
   };
+  uint4 rk, rv;   // of K of step i + 2 and V of step i, at the beginning of phase i
   // The exponents of a block, K's in the low byte.
   const int e_shift = (tiles.e_off & 2) * 8;
   auto exps_of = [&](int id) __attribute__((always_inline)) {
@@ -165,49 +164,43 @@ __device__ __forceinline__ void prefill_tile_fp8(
   };
   auto k_scale = [&](uint32_t w) { return fp8_scale((w >> e_shift) & 0xff); };
   auto v_scale = [&](uint32_t w) { return fp8_scale((w >> (e_shift + 8)) & 0xff); };
-  auto raw_read = [&](int buf, int kind) __attribute__((always_inline)) {
-    return *reinterpret_cast<const uint4*>(&lds.raw[buf][kind][0][wave * 1024 + lane_id_fresh() * 16]);
-  };
-  // K: this lane's 16 dims of one token are two 16-byte chunks of the chunk-major tile.
-  auto put_k = [&](int step, int part, uint32_t a, uint32_t b,
+  // Where the lane's converted pieces go. K: 16 dims of one token are two 16-byte
+  // chunks of the chunk-major tile. V: dword w is tokens 4 (lane / 16) .. + 4 of dim
+  // 64 half + 16 w + lane % 16, eight bytes of its row; a row's two 16-byte halves are
+  // swapped on every other group of 8.
+  const int k_at = my_kb * kTile + ((2 * (my_half * 4 + lane / 16)) * kBS + lane % 16) * 16;
+  const int v_at = my_kb * kTile + (my_half * 64 + lane % 16) * 32 +
+                   ((lane / 32) ^ ((lane >> 3) & 1)) * 16 + (lane / 16 % 2) * 8;
+  auto put_k = [&](int buf, int at, int part, uint32_t a, uint32_t b,
                    float scale) __attribute__((always_inline)) {
-    const int ln = lane_id_fresh();
-    *reinterpret_cast<bf16x8_t*>(
-        &lds.k[step % kBufs][my_kb][((2 * (my_half * 4 + ln / 16) + part) * kBS + ln % 16) * 16]) =
+    *reinterpret_cast<bf16x8_t*>(&lds.k[buf][0][at + part * kBS * 16]) =
         fp8x8_to_bf16(a, b, scale, scale);
   };
-  // V: dword w is tokens 4 (lane / 16) .. + 4 of dim 64 half + 16 w + lane % 16, eight
-  // bytes of its row; a row's two 16-byte halves are swapped on every other group of 8.
-  auto put_v = [&](int step, int w, uint32_t a, float scale) __attribute__((always_inline)) {
-    const int ln = lane_id_fresh();
-    const int t4 = ln / 16, jl = ln % 16;
-    *reinterpret_cast<uint2*>(&lds.v[step % kBufs][my_kb]
-                                    [(my_half * 64 + w * 16 + jl) * 32 +
-                                     ((t4 / 2) ^ ((jl >> 3) & 1)) * 16 + (t4 % 2) * 8]) =
-        fp8x4_to_bf16(a, scale);
+  auto put_v = [&](int buf, int at, int w, uint32_t a, float scale) __attribute__((always_inline)) {
+    *reinterpret_cast<uint2*>(&lds.v[buf][0][at + w * 512]) = fp8x4_to_bf16(a, scale);
   };
   // Whether this wavefront's V block of a step holds slots that must not contribute.
   auto v_masked = [&](int step, int id) __attribute__((always_inline)) {
     return id < 0 || step * kKeys + (my_kb + 1) * kBS > L;
   };
-  auto v_mask = [&](int step, int id, uint4& v) __attribute__((always_inline)) {
-    const int t4 = lane_id_fresh() / 16;
+  auto v_patch = [&](int step, int id) __attribute__((always_inline)) {
+    const unsigned ln = lane_id_fresh();
     const uint32_t keep =
-        id < 0 ? 0u : first_bytes(L - (step * kKeys + my_kb * kBS + t4 * 4));
-    v = make_uint4(v.x & keep, v.y & keep, v.z & keep, v.w & keep);
+        id < 0 ? 0u : first_bytes(L - (step * kKeys + my_kb * kBS + (int)(ln / 16) * 4));
+    rv = make_uint4(rv.x & keep, rv.y & keep, rv.z & keep, rv.w & keep);
   };
   auto convert_k = [&](int step, uint32_t exps) __attribute__((always_inline)) {
-    const uint4 k = raw_read(step % kBufs, 0);
-    put_k(step, 0, k.x, k.y, k_scale(exps));
-    put_k(step, 1, k.z, k.w, k_scale(exps));
+    const int buf = step % kBufs;
+    put_k(buf, k_at, 0, rk.x, rk.y, k_scale(exps));
+    put_k(buf, k_at, 1, rk.z, rk.w, k_scale(exps));
   };
   auto convert_v = [&](int step, int id, uint32_t exps) __attribute__((always_inline)) {
-    uint4 v = raw_read(step % kBufs, 1);
-    if (v_masked(step, id)) v_mask(step, id, v);
-    put_v(step, 0, v.x, v_scale(exps));
-    put_v(step, 1, v.y, v_scale(exps));
-    put_v(step, 2, v.z, v_scale(exps));
-    put_v(step, 3, v.w, v_scale(exps));
+    const int buf = step % kBufs;
+    if (v_masked(step, id)) v_patch(step, id);
+    put_v(buf, v_at, 0, rv.x, v_scale(exps));
+    put_v(buf, v_at, 1, rv.y, v_scale(exps));
+    put_v(buf, v_at, 2, rv.z, v_scale(exps));
+    put_v(buf, v_at, 3, rv.w, v_scale(exps));
   };
   auto step_clean = [&](int step, int bits) __attribute__((always_inline)) { return bits == 0xf && (step + 1) * kKeys <= L; };
 
@@ -275,7 +268,7 @@ __device__ __forceinline__ void prefill_tile_fp8(
   // wavefront's of V of step i + 1, read at the end of the phase before (ahead of its barrier)
   StepIds idsK = {{-1, -1, -1, -1}};
   int idK = -1, idV = -1;
-  // of the raw steps that the coming phase converts, K of step i + 2 and V of step
+  // of what the coming phase converts (rk, rv), K of step i + 2 and V of step
   // i: this wavefront's V block, and the words that hold their exponents
   int v_id = -1;
   uint32_t k_exps = 0, v_exps = 0;
@@ -291,12 +284,15 @@ __device__ __forceinline__ void prefill_tile_fp8(
   // As in the bf16 tile, the work is laid out by hand in 32 issue slots: slot k
   // issues matrix instruction k (p.v for k < 16, q.k after), the LDS read of the
   // operand five slots ahead, one exponential with its share of the row sum and
-  // bf16 packing, and in some slots a part of the conversion. The row max, when a
-  // step needs it, follows the slots.
-  auto phase = [&](auto qk_tag, auto pv_tag, int i, f32x16_t (&s_cur)[2],
+  // bf16 packing, and some a part of the conversion. The slots are one block without a
+  // branch, so the exponentials stay in theirs. The row max, when a step needs it,
+  // follows them.
+  // parity: i % 2, in the loop a constant, so that the buffers' addresses are too.
+  auto phase = [&](auto qk_tag, auto pv_tag, auto parity, int i, f32x16_t (&s_cur)[2],
                    f32x16_t (&s_nxt)[2], const bf16x8_t (&p_prev)[4], bf16x8_t (&p_cur)[4]) __attribute__((always_inline)) {
     constexpr bool kQK = decltype(qk_tag)::value;
     constexpr bool kPV = decltype(pv_tag)::value;
+    const int cur = parity, nxt = 1 - cur;   // buffers of steps i and i + 1
     // The block ids were read before the barrier that ends the previous
     // phase: wait for them here, while no operand read of this phase is in
     // flight, so that the operand prefetch below is never drained for them
@@ -304,9 +300,11 @@ __device__ __forceinline__ void prefill_tile_fp8(
     // order).
     __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
     if (needs_mask(i, bits & 0xf)) mask_scores(i, bits & 0xf, s_cur);
+    // here and not where it is converted, so that no branch splits the slots
+    if (v_masked(i, v_id)) v_patch(i, v_id);
 
-    const int vbuf = (i + kBufs - 1) % kBufs;     // V of step i - 1
-    const int kbuf = (i + 1) % kBufs;             // K of step i + 1
+    const int vbuf = nxt;   // V of step i - 1
+    const int kbuf = nxt;   // K of step i + 1
     auto has_mfma = [&](int k) __attribute__((always_inline)) { return k < 16 ? kPV : kQK; };
     auto a_frag = [&](int k) __attribute__((always_inline)) {
       if (k < 16)
@@ -326,17 +324,12 @@ __device__ __forceinline__ void prefill_tile_fp8(
     bool rescale = false;
     float pe[32];
     uint32_t pw[16];
-    uint4 rk = {}, rv = {};
     constexpr int kConvSlot = 6;
     const int new_k = kQK ? real(idK) : -1, new_v = kQK ? real(idV) : -1;
     if (kQK) bits |= id_bits(idsK) << 12;
     f32x16_t zero;
 #pragma unroll
     for (int e = 0; e < 16; ++e) zero[e] = 0.f;
-    // Raised issue priority while this wavefront issues its matrix slots, so
-    // that the arbiter prefers its MFMAs and operand reads over the vector
-    // work of the other wavefront of the SIMD (0.5-0.9% faster, same-box A/B).
-    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int k = 0; k < 32; ++k) {
       // operand reads for slot k + kAhead
@@ -360,24 +353,16 @@ __device__ __forceinline__ void prefill_tile_fp8(
           psum = dot2_bf16(pw[e / 2], kBf16OnePair, psum);
         }
       }
-      // the conversion: this wavefront's own gathers of the phase before have
-      // landed once its count of them is zero
-      if (k == kConvSlot) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (kQK) rk = raw_read(i % kBufs, 0);
-      }
-      if (k == kConvSlot + 6) rv = raw_read(i % kBufs, 1);
-      if (k == kConvSlot + 1 && kQK) gather2(new_k, 0, (i + 1) % kBufs, new_v, 1, (i + 1) % kBufs);
-      if (k == kConvSlot + 4 && kQK) put_k(i + 2, 0, rk.x, rk.y, k_scale(k_exps));
-      if (k == kConvSlot + 5 && kQK) put_k(i + 2, 1, rk.z, rk.w, k_scale(k_exps));
-      if (k == kConvSlot + 9 && v_masked(i, v_id)) v_mask(i, v_id, rv);
-      if (k == kConvSlot + 10) put_v(i, 0, rv.x, v_scale(v_exps));
-      if (k == kConvSlot + 12) put_v(i, 1, rv.y, v_scale(v_exps));
-      if (k == kConvSlot + 14) put_v(i, 2, rv.z, v_scale(v_exps));
-      if (k == kConvSlot + 16) put_v(i, 3, rv.w, v_scale(v_exps));
+      if (k == kConvSlot + 1 && kQK) put_k(cur, k_at, 0, rk.x, rk.y, k_scale(k_exps));
+      if (k == kConvSlot + 3 && kQK) put_k(cur, k_at, 1, rk.z, rk.w, k_scale(k_exps));
+      if (k == kConvSlot + 4 && kQK) rk = gather(new_k, tiles.k_off);
+      if (k == kConvSlot + 6) put_v(cur, v_at, 0, rv.x, v_scale(v_exps));
+      if (k == kConvSlot + 8) put_v(cur, v_at, 1, rv.y, v_scale(v_exps));
+      if (k == kConvSlot + 10) put_v(cur, v_at, 2, rv.z, v_scale(v_exps));
+      if (k == kConvSlot + 12) put_v(cur, v_at, 3, rv.w, v_scale(v_exps));
+      if (k == kConvSlot + 13 && kQK) rv = gather(new_v, tiles.v_off);
       __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_s_setprio(0);
     // A row without a reference yet, or a lane whose partial row sum (which
     // bounds each of its exponentials) left 2^8: take the exact row max, move
     // the reference of the rows that outgrew theirs by more than 2^8, and
@@ -451,15 +436,17 @@ __device__ __forceinline__ void prefill_tile_fp8(
       idK = my_entry(i0 + 3);
     }
     idV = b;
-    gather2(a, 0, i0 % kBufs, b, 0, (i0 + 1) % kBufs);
+    rk = gather(a, tiles.k_off);
+    rv = gather(b, tiles.k_off);
     const uint32_t ea = exps_of(a), eb = exps_of(b);
     k_exps = exps_of(c2);
     v_exps = ea;
     v_id = a;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     convert_k(i0, ea);
+    rk = rv;
     convert_k(i0 + 1, eb);
-    gather2(c2, 0, i0 % kBufs, a, 1, i0 % kBufs);
+    rk = gather(c2, tiles.k_off);
+    rv = gather(a, tiles.v_off);
   };
 
   if (N > i0) prologue();
@@ -472,12 +459,12 @@ __device__ __forceinline__ void prefill_tile_fp8(
       __syncthreads();
       __syncthreads();   // the others' q.k of the first step
       for (int i = i0; i < N; ++i) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         convert_k(i + 2, k_exps);
         convert_v(i, v_id, v_exps);
         if (i + 1 < N) {
           const int new_k = real(idK), new_v = real(idV);
-          gather2(new_k, 0, (i + 1) % kBufs, new_v, 1, (i + 1) % kBufs);
+          rk = gather(new_k, tiles.k_off);
+          rv = gather(new_v, tiles.v_off);
           k_exps = exps_of(new_k);
           v_exps = exps_of(new_v);
           v_id = new_v;
@@ -496,27 +483,33 @@ __device__ __forceinline__ void prefill_tile_fp8(
     __syncthreads();   // K of the first step is read; its pipeline step writes its buffer
     constexpr std::true_type T{};
     constexpr std::false_type F{};
+    constexpr std::integral_constant<int, 0> even{};
+    constexpr std::integral_constant<int, 1> odd{};
     if (i0 + 1 < N)
-      phase(T, F, i0, sA, sB, pB, pA);
+      phase(T, F, even, i0, sA, sB, pB, pA);
     else
-      phase(F, F, i0, sA, sB, pB, pA);
+      phase(F, F, even, i0, sA, sB, pB, pA);
     int i = i0 + 1;   // i0 is even: even steps use sA and pA
     for (; i + 1 <= N - 2; i += 2) {
-      phase(T, T, i, sB, sA, pA, pB);
-      phase(T, T, i + 1, sA, sB, pB, pA);
+      phase(T, T, odd, i, sB, sA, pA, pB);
+      phase(T, T, even, i + 1, sA, sB, pB, pA);
     }
     if (i <= N - 2) {
-      phase(T, T, i, sB, sA, pA, pB);
+      phase(T, T, odd, i, sB, sA, pA, pB);
       ++i;
     }
-    // p.v of the last step (its V was converted in the last phase)
+    // The last step, in one form whatever its parity (as two, the registers of both
+    // would be live together).
     if (i0 + 1 < N) {
-      if (i & 1)
-        phase(F, T, i, sB, sA, pA, pB);
-      else
-        phase(F, T, i, sA, sB, pB, pA);
+      if (i & 1) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) sA[k] = sB[k];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) pB[k] = pA[k];
+      }
+      phase(F, T, i & 1, i, sA, sB, pB, pA);
     }
-    pv(N - 1, ((N - 1) & 1) ? pB : pA);
+    pv(N - 1, pA);   // its V was converted in the last phase
   }
 
   // ---- write O (this lane: row lm): normalised, or the item's partial ----
@@ -529,14 +522,14 @@ __device__ __forceinline__ void prefill_tile_fp8(
     if (__builtin_amdgcn_readfirstlane(end.slot) < 0) {
       // A lane holds 8-byte pieces of its row, two lanes per row: stored like
       // that, an instruction touches 32 rows of 16 bytes. Half the dims at a
-      // time go through the wavefront's part of the raw and K buffers, which
-      // nobody reads any more, and are stored in runs of 128 bytes. A call, stored directly and
+      // time go through the wavefront's part of the K buffers and more,
+      // which nobody reads any more, and are stored in runs of 128 bytes. A call, stored directly and
       // like this: 7 fresh prompts of 188 to 2031 rows (64 query heads over 8)
       // 172 -> 159 us, 64 of 100 rows (32 over 8) 59 -> 51 us, 4 of 64 rows 12.8 ->
       // 10.6 us; tiles of hundreds of steps do not notice.
       constexpr int kHalf = kD / 2, kRowBytes = kHalf * 2 + 16;   // padded against conflicts
-      static_assert(kWaves * 32 * kRowBytes <= (int)(sizeof(lds.raw) + sizeof(lds.k)), "fits");
-      uint8_t* stage = reinterpret_cast<uint8_t*>(&lds) + wave * 32 * kRowBytes;
+      static_assert(kWaves * 32 * kRowBytes <= (int)(sizeof(lds.k) + sizeof(lds.more)), "fits");
+      uint8_t* stage = &lds.k[0][0][0] + wave * 32 * kRowBytes;
       const float inv = lt > 0.f ? 1.f / lt : 0.f;
       const int sr = lane / 16, sc = lane % 16;   // row of four, 8-byte piece of its half
 #pragma unroll
