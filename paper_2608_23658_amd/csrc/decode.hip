@@ -75,6 +75,21 @@
 // long sequences have. The G query heads sharing the kv head are served by
 // every K/V byte read (grouped-query sharing).
 //
+// With the cache in 8 bits a block's exponents are one line for all its heads, 3% of the
+// traffic if each head's XCD fetches it. There the heads of a (sequence, split) go
+// to one XCD, one after another, and eight of those at a time to the eight XCDs,
+// turned by one step or more from group to group so that neither a long sequence's
+// splits nor a split of all sequences gather on a few. Up to kXcdBlocks
+// workgroups, where that could leave XCDs uneven, the order is as above. Per call,
+// heads over the XCDs / on one (32 query heads over 8, head_dim 128):
+//   64 sequences of 1000 to 4000        66.5 / 59.0 us
+//   256 of 512 to 4096                 211.7 / 208.9 us (rocprof: 205 / 203)
+//   131071, 65535 and 4 of 700 to 4796  85.5 / 77.2 us
+//   1 of 60000                          30.6 / 27.5 us
+//   24 of 500 to 4000                   31.4 / 29.9 us
+//   128 of 500 to 5000, 64 over 8, d 64 75.8 / 70.0 us
+//   6 of 1000 to 8000 (384 workgroups)  18.7 / 20.1 us, so not taken
+//
 // A wavefront walks its share in steps of 64 tokens (4 blocks of 16). Each
 // block's K tile and V tile are read as they lie in memory, 1 KiB per 16-byte
 // load (K and V are read once, so the loads are non-temporal), and the K and V
@@ -109,6 +124,7 @@ constexpr long long kAheadBlocks = 1024;
 constexpr long long kFullBlocks = 8192, kHalfBlocks = 16384, kMostBlocks = 32768;
 constexpr long long kMinPieces = 48;
 constexpr int kShortSteps = 6, kShortBlocks = 1024;   // fp32
+constexpr int kXcds = 8, kXcdBlocks = 384;            // 8 bits
 
 // Orders a wavefront's LDS writes before its own later reads by other lanes.
 __device__ __forceinline__ void wave_lds_sync() {
@@ -312,9 +328,18 @@ void decode_split_kernel(
   using S = DecodeShape<D, BF16>;
   constexpr int W = kDecodeWaves;
   const int wid = blockIdx.x;
-  const int g = wid % num_kv_heads;
-  const int s = (wid / num_kv_heads) % num_seqs;
-  const int piece = wid / (num_kv_heads * num_seqs);
+  int g = wid % num_kv_heads;
+  int unit = wid / num_kv_heads;   // sequence, then piece
+  if constexpr (kFp8) {
+    const int whole = gridDim.x / (kXcds * num_kv_heads) * (kXcds * num_kv_heads);
+    if (gridDim.x > kXcdBlocks && wid < whole) {
+      const int k = wid / kXcds, j = k / num_kv_heads;
+      g = k % num_kv_heads;
+      unit = j * kXcds + (wid + j + j / 8 + j / 64) % kXcds;
+    }
+  }
+  const int s = unit % num_seqs;
+  const int piece = unit / num_seqs;
   const int wave =
       kSpread ? piece % W : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int h0 = g * G;
