@@ -135,10 +135,13 @@ def append(raw: np.ndarray, k_new: np.ndarray, v_new: np.ndarray, slot_mapping, 
 
 
 def to_bf16_layer(raw: np.ndarray, num_kv_heads: int, head_dim: int) -> np.ndarray:
-    """The layer's values as bf16 bit patterns (uint16) in the bf16 layout; exact."""
+    """The layer's values as bf16 bit patterns (uint16) in the bf16 layout; exact. Tiles whose
+    exponent is none in use become NaN."""
     lay = Layer(raw, num_kv_heads, head_dim)
     n = len(lay.raw)
-    codes = decode(lay.codes) * np.exp2(lay.exps.transpose(0, 2, 1)[..., None] - 127.0)
+    exps = lay.exps.transpose(0, 2, 1)[..., None] - 127.0
+    exps = np.where((exps < E_MIN) | (exps > E_MAX), np.nan, exps)   # of a block never begun
+    codes = decode(lay.codes) * np.exp2(exps)
     r, j = np.arange(BS)[:, None], np.arange(head_dim)[None, :]
     out = np.empty((n, 2, num_kv_heads, BS * head_dim), np.float64)
     to = ((j // 8 * BS + r) * 8 + j % 8, j * BS + r)

@@ -18,7 +18,14 @@
 //
 // A workgroup of four wavefronts has the runs that begin in a window of the list.
 // A window of 32 tokens of a chunk is two runs, K and V of each a wavefront's; the tokens of a
-// decode step are a run each, and a window of 2 spreads them over the CUs.
+// decode step are a run each, and a window of 2 spreads them over the CUs. Only the
+// device knows which it is, so the window goes by the number of tokens. bf16, 8 heads of
+// 128 (rocprof, us), windows of 2 / 8 / 32:
+//   tokens            256               512              2048              8192
+//   one a block   5.3 / 8.2 / 22.9  7.8 / 9.0 / 23.2  22.6 / 19.5 / 27.0  88 / 71 / 72
+//   one chunk     4.2 / 3.8 /  5.0  5.2 / 4.1 /  5.0  12.3 /  6.8 /  5.8  39 / 17 / 11.5
+// A chunk of 8192 moves 50 MB, 10.6 us at the rate of a large copy. A token alone
+// touches all 16 lines of its V tile, 4 tokens x 4 dims to 16 bytes, with a byte each.
 
 #include "common.hpp"
 #include "kv_fp8.hpp"
@@ -29,8 +36,9 @@ namespace kvattn {
 namespace {
 constexpr int kBS = 16;
 constexpr int kAppendWaves = 4;
-constexpr int kSmallTokens = 1024;   // up to here windows of kSmallWindow tokens
-constexpr int kSmallWindow = 2, kWindow = 32;
+constexpr int kWindow = 32;                     // tokens of a window
+constexpr int kFewTokens = 512, kFewWindow = 2;    // up to kFewTokens tokens
+constexpr int kSomeTokens = 2048, kSomeWindow = 8; // up to kSomeTokens
 static_assert(kWindow + kBS <= kWave, "a window's slots and those its last run may reach");
 
 typedef short s16x2_t __attribute__((ext_vector_type(2)));
@@ -298,13 +306,14 @@ __global__ __launch_bounds__(kAppendWaves * kWave) void kv_append_fp8_kernel(
 
 template <int ESZ, int D>
 static hipError_t launch_append_fp8_t(const AppendArgs& a) {
-  const bool small = a.num_tokens <= kSmallTokens;
-  const int win = small ? kSmallWindow : kWindow;
+  const bool few = a.num_tokens <= kFewTokens, some = a.num_tokens <= kSomeTokens;
+  const int win = few ? kFewWindow : some ? kSomeWindow : kWindow;
   const long long blocks = ((long long)a.num_tokens + win - 1) / win * a.num_kv_heads;
   if (blocks == 0) return hipSuccess;
   if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-  auto kernel = small ? kv_append_fp8_kernel<ESZ, D, kSmallWindow>
-                      : kv_append_fp8_kernel<ESZ, D, kWindow>;
+  auto kernel = few    ? kv_append_fp8_kernel<ESZ, D, kFewWindow>
+                : some ? kv_append_fp8_kernel<ESZ, D, kSomeWindow>
+                       : kv_append_fp8_kernel<ESZ, D, kWindow>;
   trace_before(a.stream, "kv_append_fp8");
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kAppendWaves * kWave), 0, a.stream,
                      static_cast<const uint8_t*>(a.k_new), static_cast<const uint8_t*>(a.v_new),

@@ -8,10 +8,15 @@
 //   new entries of its table: [ceil(c_s / 16), ceil((c_s + n_s) / 16)), the ids
 //   from place sum over requests before s of their count
 // Two sums over the requests, one after the other since the second counts what
-// the first has cut. Bound by latency: one launch, in which every workgroup does the
-// sums for itself (requests in tiles of 4096, one tile in nearly every call)
-// and then writes its share of the tile's requests and tokens, finding a
-// token's request by a search in LDS.
+// the first has cut; the first saturates at max_tokens, which is associative and stays
+// below 32 bits. Bound by latency: one launch, in which every workgroup does the
+// sums for itself (requests in tiles, one tile in nearly every call)
+// and then writes its share of the tile's requests and tokens, finding a token's
+// request by a search in LDS. A thread per token, in up to 64 workgroups: 2048 requests
+// with 24 prompts and 16384 tokens took 11.1 / 9.2 / 7.9 us at 4 / 2 / 1 tokens a
+// thread, 7.0 with workgroups of 512 threads instead of 1024, and 5.4 without reading
+// the partial blocks' ids ahead for all requests (rocprof). 256 requests of one token
+// each take 3.5 us with 256 threads (5.9 with 1024); an empty kernel takes about 2.
 
 #include <algorithm>
 
@@ -22,115 +27,137 @@ namespace kvattn {
 
 namespace {
 constexpr int kBS = 16;
-constexpr int kMapThreads = 1024;
-constexpr int kPer = 4;                          // requests per thread and tile
-constexpr int kMapTile = kMapThreads * kPer;
-constexpr int kTokensPerGroup = 2048;            // tokens for which a workgroup is added
-constexpr int kMostGroups = 64;                  // per tile
+constexpr int kPer = 4;                    // requests per thread and tile
+constexpr int kFewThreads = 256, kManyThreads = 512;
+constexpr int kMostGroups = 64;            // workgroups per tile
 
-// Exclusive sum over the workgroup of one value per thread, and the total.
-__device__ __forceinline__ long long group_scan(long long v, long long* lds, long long* total) {
+// Sums over the lanes up to this one, at most cap; x and cap below 2^31. Four steps within
+// rows of 16 lanes, then each row's total to the rows behind it.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ uint32_t scan_step(uint32_t x, uint32_t cap) {
+  return min(x + (uint32_t)__builtin_amdgcn_update_dpp(0, x, kCtrl, kRows, 0xf, false), cap);
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x, uint32_t cap) {
+  x = scan_step<0x111, 0xf>(x, cap);   // row_shr 1, 2, 4, 8
+  x = scan_step<0x112, 0xf>(x, cap);
+  x = scan_step<0x114, 0xf>(x, cap);
+  x = scan_step<0x118, 0xf>(x, cap);
+  x = scan_step<0x142, 0xa>(x, cap);   // row_bcast 15 into rows 1 and 3
+  return scan_step<0x143, 0xc>(x, cap);   // row_bcast 31 into rows 2 and 3
+}
+
+// The sum over the threads before this one, and over all, at most cap.
+template <int kThreads>
+__device__ __forceinline__ uint32_t group_scan(uint32_t v, uint32_t cap, uint32_t* lds,
+                                               uint32_t* total) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  long long x = v;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const long long y = __shfl_up(x, o, kWave);
-    x += lane >= o ? y : 0;
-  }
+  const uint32_t x = wave_scan(v, cap);
   if (lane == kWave - 1) lds[wave] = x;
   __syncthreads();
-  long long before = 0, all = 0;
+  uint32_t before = 0, all = 0;
 #pragma unroll
-  for (int w = 0; w < kMapThreads / kWave; ++w) {
-    before += w < wave ? lds[w] : 0;
-    all += lds[w];
+  for (int w = 0; w < kThreads / kWave; ++w) {
+    const uint32_t y = lds[w];
+    before = min(before + (w < wave ? y : 0), cap);
+    all = min(all + y, cap);
   }
   __syncthreads();
   *total = all;
-  return before + x - v;
+  const uint32_t left = __shfl_up(x, 1, kWave);
+  return lane ? min(before + left, cap) : before;
 }
 }  // namespace
 
-__global__ __launch_bounds__(kMapThreads) void step_map_kernel(StepMapArgs a, int tiles,
-                                                               int groups) {
-  __shared__ int cu[kMapTile + 1], cached[kMapTile], ids_at[kMapTile];
-  __shared__ long long scan[kMapThreads / kWave];
+template <int kThreads>
+__global__ __launch_bounds__(kThreads) void step_map_kernel(StepMapArgs a, int tiles, int groups) {
+  constexpr int kTile = kThreads * kPer;
+  __shared__ int cu[kTile + 1], cached[kTile], ids_at[kTile];
+  __shared__ uint32_t scan[kThreads / kWave];
   const int tid = threadIdx.x;
   const int my_tile = blockIdx.x / groups, group = blockIdx.x % groups;
-  const long long room = (long long)a.max_blocks * kBS;
-  long long tokens = 0, ids = 0;                 // of the tiles before
+  const int room = a.max_blocks * kBS;
+  const uint32_t most = a.max_tokens;
+  constexpr uint32_t kNoCap = 0x7fffffff;
+  uint32_t tokens = 0, ids = 0;                  // of the tiles before
   int base = 0;
   for (int tile = 0;; ++tile) {
-    base = tile * kMapTile;
-    int c[kPer];
-    long long n[kPer], sum = 0, total;
+    base = tile * kTile;
+    int c[kPer], held[kPer], own[kPer];
+    uint32_t n[kPer], sum = 0, total;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
-      const int s = base + tid * kPer + k;
+      const int s = base + k * kThreads + tid;   // coalesced; by thread from LDS below
       c[k] = s < a.num_seqs ? max(a.cached[s], 0) : 0;
       const int w = s < a.num_seqs ? a.wanted[s] : 0;
-      n[k] = max(min((long long)max(w, 0), room - c[k]), 0ll);
-      sum += n[k];
+      cu[k * kThreads + tid] = min(max(w, 0), max(room - c[k], 0));
+      cached[k * kThreads + tid] = c[k];
     }
-    long long at = tokens + group_scan(sum, scan, &total);
-    int new_ids = 0;
-    int first[kPer], took[kPer];
+    __syncthreads();
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
-      first[k] = (int)min(at, (long long)a.max_tokens);
-      at += n[k];
-      took[k] = (int)min(at, (long long)a.max_tokens) - first[k];
-      new_ids += (int)(((long long)c[k] + took[k] + kBS - 1) / kBS - ((long long)c[k] + kBS - 1) / kBS);
+      c[k] = cached[tid * kPer + k];
+      held[k] = (int)(((uint32_t)c[k] + kBS - 1) / kBS);
+      n[k] = min((uint32_t)cu[tid * kPer + k], most);
+      sum = min(sum + n[k], most);
     }
-    tokens += total;
-    long long id_at = ids + group_scan(new_ids, scan, &total);
+    uint32_t at = min(tokens + group_scan<kThreads>(sum, most, scan, &total), most);
+    tokens = min(tokens + total, most);
+    uint32_t new_ids = 0, first[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      first[k] = at;
+      at = min(at + n[k], most);
+      own[k] = (int)(((uint32_t)c[k] + (at - first[k]) + kBS - 1) / kBS) - held[k];
+      new_ids += own[k];
+    }
+    uint32_t id_at = ids + group_scan<kThreads>(new_ids, kNoCap, scan, &total);
     ids += total;
     if (tile < my_tile) continue;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
       const int i = tid * kPer + k;
       cu[i] = first[k];
-      cached[i] = c[k];
-      ids_at[i] = (int)min(id_at, (long long)0x7fffffff);
-      id_at += ((long long)c[k] + took[k] + kBS - 1) / kBS - ((long long)c[k] + kBS - 1) / kBS;
+      ids_at[i] = id_at;
+      id_at += own[k];
     }
-    if (tid == 0) cu[kMapTile] = (int)min(tokens, (long long)a.max_tokens);
+    if (tid == 0) cu[kTile] = tokens;
     break;
   }
   __syncthreads();
 
   // ---- the tile's requests ----
-  const int here = min(kMapTile, a.num_seqs - base);
-  for (int i = group * kMapThreads + tid; i < here; i += groups * kMapThreads) {
+  const int here = min(kTile, a.num_seqs - base);
+  for (int i = group * kThreads + tid; i < here; i += groups * kThreads) {
     a.seq_lens[base + i] = cached[i] + cu[i + 1] - cu[i];
     a.cu_seqlens_q[base + i] = cu[i];
   }
-  const int end = cu[kMapTile];
+  const int end = cu[kTile];
   const bool last = my_tile == tiles - 1;
   if (last && group == 0 && tid == 0) {
     a.cu_seqlens_q[a.num_seqs] = end;
     a.used[0] = end;
-    a.used[1] = (int)min(ids, (long long)0x7fffffff);
+    a.used[1] = ids;
   }
 
   // ---- its tokens; the first token of a new block writes the block's entry ----
-  const int stride = groups * kMapThreads;
-  for (int t = cu[0] + group * kMapThreads + tid; t < end; t += stride) {
+  const int stride = groups * kThreads;
+  for (long long tl = (long long)cu[0] + group * kThreads + tid; tl < end; tl += stride) {
+    const int t = (int)tl;
     int lo = 0, hi = here - 1;                   // last request with cu <= t: it has t
     while (lo < hi) {
       const int mid = (lo + hi + 1) / 2;
       if (cu[mid] <= t) lo = mid; else hi = mid - 1;
     }
     const int pos = cached[lo] + t - cu[lo];
-    const int held = (int)(((long long)cached[lo] + kBS - 1) / kBS);
+    const int held = (int)(((uint32_t)cached[lo] + kBS - 1) / kBS);
     const int entry = pos / kBS;
     int* row = a.block_table + (size_t)(base + lo) * a.max_blocks;
     int id;
-    if (entry < held) {
+    if (entry < held) {   // the partial block the request holds
       id = row[entry];
     } else {
-      const long long place = (long long)ids_at[lo] + entry - held;
-      id = place < a.num_free ? a.free_ids[place] : -1;
+      const uint32_t place = (uint32_t)ids_at[lo] + entry - held;
+      id = place < (uint32_t)a.num_free ? a.free_ids[place] : -1;
       if (pos % kBS == 0) row[entry] = id;
     }
     a.slot_mapping[t] = id >= 0 && id <= (0x7fffffff - (kBS - 1)) / kBS ? id * kBS + pos % kBS : -1;
@@ -138,19 +165,29 @@ __global__ __launch_bounds__(kMapThreads) void step_map_kernel(StepMapArgs a, in
   }
   // ---- rows of the step that no token has ----
   if (!last) return;
-  for (long long t = (long long)end + group * kMapThreads + tid; t < a.max_tokens; t += stride) {
+  for (long long t = (long long)end + group * kThreads + tid; t < a.max_tokens; t += stride) {
     a.slot_mapping[t] = -1;
     a.positions[t] = 0;
   }
 }
 
-hipError_t launch_step_map(const StepMapArgs& a) {
-  const int tiles = std::max(1, (a.num_seqs + kMapTile - 1) / kMapTile);
+template <int kThreads>
+static void launch_step_map_t(const StepMapArgs& a) {
+  constexpr int kTile = kThreads * kPer;
+  const int tiles = std::max(1, (a.num_seqs + kTile - 1) / kTile);
   const int groups =
-      std::min(kMostGroups, std::max(1, (a.max_tokens + kTokensPerGroup - 1) / kTokensPerGroup));
+      std::min(kMostGroups, std::max(1, (int)(((long long)a.max_tokens + kThreads - 1) /
+                                              kThreads)));
+  hipLaunchKernelGGL(step_map_kernel<kThreads>, dim3(tiles * groups), dim3(kThreads), 0, a.stream,
+                     a, tiles, groups);
+}
+
+hipError_t launch_step_map(const StepMapArgs& a) {
   trace_before(a.stream, "step_map");
-  hipLaunchKernelGGL(step_map_kernel, dim3(tiles * groups), dim3(kMapThreads), 0, a.stream, a, tiles,
-                     groups);
+  if (a.num_seqs <= kFewThreads * kPer)
+    launch_step_map_t<kFewThreads>(a);
+  else
+    launch_step_map_t<kManyThreads>(a);
   trace_after(a.stream);
   return hipGetLastError();
 }

@@ -367,13 +367,18 @@ def kv_append(k_new: torch.Tensor, v_new: torch.Tensor, slot_mapping: torch.Tens
     check(rc)
 
 
-def _require_current_device(*ts):
-    """Launches go to the current device: tensors of another one are refused."""
-    cur = torch.cuda.current_device()
+def _require_here(*ts):
+    """Tensors reach the library as bare pointers and launches go to the current
+    device: they must be contiguous, on the GPU, and on that one. (One pass when all is
+    well: a small call is bound by the time this module takes.)"""
+    cur = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2   # CPU: -1
     for t in ts:
-        if isinstance(t, torch.Tensor) and t.device.index != cur:
-            raise ValueError(f"tensors must be on the current device (cuda:{cur}), "
-                             f"not {t.device}")
+        if isinstance(t, torch.Tensor) and (t.get_device() != cur or not t.is_contiguous()):
+            _require_cuda(*ts)
+            cur = torch.cuda.current_device()
+            if t.get_device() != cur:
+                raise ValueError(f"tensors must be on the current device (cuda:{cur}), "
+                                 f"not {t.device}")
 
 
 def _for_stream(stream, *ts):
@@ -395,7 +400,8 @@ def fp8_block_bytes(num_kv_heads: int, head_dim: int) -> int:
 def _require_fp8_layer(kv_layer, num_blocks: int, num_kv_heads: int, head_dim: int):
     if isinstance(kv_layer, torch.Tensor):
         have = kv_layer.numel() * kv_layer.element_size()
-        need = int(num_blocks) * fp8_block_bytes(num_kv_heads, head_dim)
+        need = int(num_blocks) * (2 * num_kv_heads * 16 * head_dim +
+                                  (2 * num_kv_heads + 127) // 128 * 128)
         if have < need:
             raise ValueError(f"kv_layer has {have} bytes, {num_blocks} blocks need {need}")
 
@@ -411,8 +417,7 @@ def kv_append_fp8(k_new: torch.Tensor, v_new: torch.Tensor, slot_mapping: torch.
         raise ValueError("slot_mapping must be int32 [num_tokens]")
     code = _dtype_code(k_new.dtype)
     _require_fp8_layer(kv_layer, num_blocks, Hkv, d)
-    _require_cuda(k_new, v_new, slot_mapping, kv_layer)
-    _require_current_device(k_new, v_new, slot_mapping, kv_layer)
+    _require_here(k_new, v_new, slot_mapping, kv_layer)
     check(lib().kvattn_kv_append_fp8(k_new.data_ptr(), v_new.data_ptr(), slot_mapping.data_ptr(),
                                      _ptr(kv_layer), int(num_blocks), T, Hkv, d, int(block_size),
                                      code, _stream(stream)))
@@ -429,8 +434,7 @@ def decode_fp8(q: torch.Tensor, kv_layer, num_blocks: int, block_table: torch.Te
     _require_out(out, q)
     code = _dtype_code(q.dtype)
     _require_fp8_layer(kv_layer, num_blocks, num_kv_heads, d)
-    _require_cuda(q, kv_layer, block_table, seq_lens, out, ws)
-    _require_current_device(q, kv_layer, block_table, seq_lens, out, ws)
+    _require_here(q, kv_layer, block_table, seq_lens, out, ws)
     if out is None:
         out = torch.empty_like(q)
         _for_stream(stream, out)
@@ -460,8 +464,7 @@ def prefill_chunk_fp8(q: torch.Tensor, kv_layer, num_blocks: int, block_table: t
     _require_out(out, q)
     code = _dtype_code(q.dtype)
     _require_fp8_layer(kv_layer, num_blocks, num_kv_heads, d)
-    _require_cuda(q, kv_layer, block_table, seq_lens, cu_seqlens_q, out, ws)
-    _require_current_device(q, kv_layer, block_table, seq_lens, cu_seqlens_q, out, ws)
+    _require_here(q, kv_layer, block_table, seq_lens, cu_seqlens_q, out, ws)
     if out is None:
         out = torch.empty_like(q)
         _for_stream(stream, out)
@@ -492,8 +495,9 @@ class StepMap(NamedTuple):
     def empty(num_seqs: int, max_tokens: int, device=None) -> "StepMap":
         """Room for the maps of a step, to be kept and passed as ``out``."""
         sizes = [num_seqs, num_seqs + 1, max_tokens, max_tokens, 2]
-        return StepMap(*torch.empty(sum(sizes), dtype=torch.int32,
-                                    device=device if device is not None else "cuda").split(sizes))
+        buf = torch.empty(sum(sizes), dtype=torch.int32,
+                          device=device if device is not None else "cuda")
+        return StepMap(*torch.split_with_sizes(buf, sizes))
 
 
 def step_map(cached_lens: torch.Tensor, new_lens: torch.Tensor, free_ids: torch.Tensor,
@@ -502,26 +506,30 @@ def step_map(cached_lens: torch.Tensor, new_lens: torch.Tensor, free_ids: torch.
     """The maps of a step from the requests' lengths (``cached_lens`` and ``new_lens``
     [num_seqs] int32); new entries of ``block_table`` [num_seqs, max_blocks] take the ids of
     ``free_ids`` in order. ``out.used[1]`` counts the ids taken."""
-    S = int(cached_lens.shape[0])
-    _require_int32(cached_lens=cached_lens, new_lens=new_lens, free_ids=free_ids,
-                   block_table=block_table)
-    if cached_lens.dim() != 1 or new_lens.shape != cached_lens.shape or free_ids.dim() != 1:
-        raise ValueError("cached_lens and new_lens must be [num_seqs], free_ids one-dimensional")
-    if block_table.shape[0] != S:
+    S, MB = len(cached_lens), block_table.shape[-1]
+    i32 = torch.int32
+    if not (cached_lens.dtype is i32 and new_lens.dtype is i32 and free_ids.dtype is i32 and
+            block_table.dtype is i32 and block_table.shape == (S, MB) and free_ids.dim() == 1 and
+            cached_lens.shape == new_lens.shape == (S,)):
+        _require_int32(cached_lens=cached_lens, new_lens=new_lens, free_ids=free_ids,
+                       block_table=block_table)
+        if cached_lens.dim() != 1 or new_lens.shape != cached_lens.shape or free_ids.dim() != 1:
+            raise ValueError("cached_lens and new_lens must be [num_seqs], free_ids "
+                             "one-dimensional")
         raise ValueError(f"block_table must have {S} rows, not {block_table.shape[0]}")
-    if out is not None:
-        want = (S, S + 1, max_tokens, max_tokens, 2)
-        if any(t.dtype != torch.int32 or tuple(t.shape) != (n,) for t, n in zip(out, want)):
-            raise ValueError("out must be int32 tensors as StepMap.empty(num_seqs, max_tokens)")
-    _require_cuda(cached_lens, new_lens, free_ids, block_table, *(out or ()))
-    _require_current_device(cached_lens, new_lens, free_ids, block_table, *(out or ()))
     if out is None:
+        _require_here(cached_lens, new_lens, free_ids, block_table)
         out = StepMap.empty(S, max_tokens, block_table.device)
         _for_stream(stream, *out)
+    else:
+        want = (S, S + 1, max_tokens, max_tokens, 2)
+        if any(t.dtype != i32 or tuple(t.shape) != (n,) for t, n in zip(out, want)):
+            raise ValueError("out must be int32 tensors as StepMap.empty(num_seqs, max_tokens)")
+        _require_here(cached_lens, new_lens, free_ids, block_table, *out)
     check(lib().kvattn_step_map(cached_lens.data_ptr(), new_lens.data_ptr(), S,
                                 free_ids.data_ptr(), int(free_ids.numel()),
-                                block_table.data_ptr(), int(block_table.shape[1]),
-                                int(block_size), int(max_tokens), out.seq_lens.data_ptr(),
+                                block_table.data_ptr(), MB, int(block_size),
+                                int(max_tokens), out.seq_lens.data_ptr(),
                                 out.cu_seqlens_q.data_ptr(), out.slot_mapping.data_ptr(),
                                 out.positions.data_ptr(), out.used.data_ptr(), _stream(stream)))
     return out

@@ -69,7 +69,7 @@ def test_chunk(dtype, hkv, d, T, start):
 
 
 @pytest.mark.parametrize("dtype,hkv,d", SHAPES[:3])
-@pytest.mark.parametrize("T", [5, 256, 1500])
+@pytest.mark.parametrize("T", [5, 256, 1500, 2200])
 def test_scattered(dtype, hkv, d, T):
     """One token per block at any place in it, with padding and slots past the layer."""
     say("append fp8 scattered", dtype, hkv, d, T)
@@ -84,7 +84,7 @@ def test_scattered(dtype, hkv, d, T):
     _check(_layer(nb, hkv, d, T), k, v, slots, hkv, d)
 
 
-@pytest.mark.parametrize("T", [900, 2000])
+@pytest.mark.parametrize("T", [400, 900, 2600])
 def test_runs_of_every_length(T):
     """Ragged pieces of sequences, in pieces of 1 to 40 tokens from any slot on; windows
     of the list begin anywhere in them."""

@@ -50,6 +50,7 @@ def _random(seed, S, MB, hi_new, most=None):
 @pytest.mark.parametrize("S,MB,hi,T", [
     (1, 4, 1, 1), (1, 64, 1000, 1024), (3, 7, 40, 50), (256, 32, 1, 256), (257, 33, 90, 5000),
     (1000, 20, 17, 100), (4096, 5, 9, 20000), (4097, 5, 9, 20001), (9001, 3, 6, 30000),
+    (1024, 6, 30, 9000), (1025, 6, 30, 9000), (2048, 5, 9, 9000), (2049, 5, 9, 9000),
 ])
 def test_against_the_oracle(S, MB, hi, T):
     say("step map", S, MB, hi, T)
