@@ -89,6 +89,10 @@
 //   24 of 500 to 4000                   31.4 / 29.9 us
 //   128 of 500 to 5000, 64 over 8, d 64 75.8 / 70.0 us
 //   6 of 1000 to 8000 (384 workgroups)  18.7 / 20.1 us, so not taken
+// Its walk that loads ahead is taken further, a step's loads being half as large: at
+// head_dim 128, one workgroup per CU, up to 256 workgroups (160: 15.4 -> 13.3, 224:
+// 16.3 -> 14.2, 512: 22.0 -> 23.7 us), at head_dim 64 up to 4096 (1536: 24.2 -> 19.7,
+// 2048: 37.2 -> 33.5, 4096: 64.5 -> 63.6).
 //
 // A wavefront walks its share in steps of 64 tokens (4 blocks of 16). Each
 // block's K tile and V tile are read as they lie in memory, 1 KiB per 16-byte
@@ -125,6 +129,7 @@ constexpr long long kFullBlocks = 8192, kHalfBlocks = 16384, kMostBlocks = 32768
 constexpr long long kMinPieces = 48;
 constexpr int kShortSteps = 6, kShortBlocks = 1024;   // fp32
 constexpr int kXcds = 8, kXcdBlocks = 384;            // 8 bits
+constexpr long long kAheadBlocks64 = 4096, kAheadBlocks128 = 256;
 
 // Orders a wavefront's LDS writes before its own later reads by other lanes.
 __device__ __forceinline__ void wave_lds_sync() {
@@ -657,8 +662,9 @@ static hipError_t launch_decode_t(const DecodeArgs& a) {
   if constexpr (kCanSpread) {
     if (spread)
       split = decode_split_kernel<D, G, BF16, kTwo, true, true, false, kFp8>;
-    else if constexpr (D == 64)
-      if (max_splits > 1 && !turns && blocks <= kAheadBlocks)
+    else if constexpr (D == 64 || kFp8)
+      if (max_splits > 1 && !turns &&
+          blocks <= (!kFp8 ? kAheadBlocks : D == 64 ? kAheadBlocks64 : kAheadBlocks128))
         split = decode_split_kernel<D, G, BF16, kTwo, true, false, false, kFp8>;
   }
   trace_before(a.stream, kTwo ? "decode_split_two_tensor"

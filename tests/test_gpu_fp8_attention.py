@@ -45,6 +45,19 @@ def test_decode_by_launch(lens, bound, d):
     assert_close(out, *expected(b, True), f"decode fp8 {len(lens)} under {bound}, {d}")
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(12, 3, 128), (32, 8, 128), (8, 2, 64), (40, 5, 64)])
+def test_decode_many(hq, hkv, d):
+    """Enough workgroups that heads are placed by XCD, with some left over."""
+    lens = np.random.default_rng(hkv).integers(1, 1500, 117).tolist() + [0, 3000]
+    b, raw = fp8_batch(lens, [0 if n == 0 else 1 for n in lens], hq=hq, hkv=hkv, d=d, seed=hkv)
+    dev = Dev8(b, raw)
+    i = lens.index(0)                      # decode has a row for the empty sequence too
+    q = torch.cat([b.q[:i], torch.ones(1, hq, d, dtype=torch.bfloat16), b.q[i:]])
+    b.q, dev.q = q, q.cuda()
+    say("decode fp8 many", hq, hkv, d)
+    assert_close(dev.decode(), *expected(b, True), f"decode fp8 many {hq}/{hkv}/{d}")
+
+
 @pytest.mark.parametrize("hq,hkv", [(32, 8), (8, 8), (16, 8), (64, 8), (12, 3)])
 def test_prefill_ragged(hq, hkv):
     lens = [1, 16, 17, 64, 65, 130, 300, 700, 1025]
