@@ -265,8 +265,10 @@ int kvattn_kv_append(const void* k_new, const void* v_new, const int32_t* slot_m
  * are rounded to the new scale (exact but for those that leave e4m3's normal range, below
  * 2^-14 of the largest value). Values are rounded to nearest even; NaN and
  * infinities become NaN, finite values beyond 448 * 2^119 the largest code. Skipped
- * slots, alignment and repeated slots as for kvattn_kv_append; a block whose tokens stand
- * in several places of one call's list has unspecified contents.
+ * slots and alignment as for kvattn_kv_append. A block with a repeated slot, or whose
+ * tokens stand in several places of one call's list (a skipped slot between them
+ * parts them too), has unspecified contents; other blocks are not touched. k_new and v_new
+ * must not overlap the layer.
  * Supported: head_dim 64 and 128, block_size 16.
  *
  * kvattn_decode_fp8, kvattn_prefill_chunk_fp8: kvattn_decode and

@@ -339,13 +339,11 @@ extern "C" size_t kvattn_prefill_workspace_bytes(int num_seqs, int total_q_token
 
 namespace {
 int prefill_common(const char* fn, bool fp8, const void* q, const void* kv_layer, int num_blocks,
-                                    const int32_t* block_table, const int32_t* seq_lens,
-                                    const int32_t* cu_seqlens_q, void* out, int num_seqs,
-                                    int total_q_tokens, int max_num_batched_tokens,
-                                    int num_q_heads, int num_kv_heads, int head_dim,
-                                    int block_size, int max_blocks_per_seq, int max_seq_len,
-                                    float scale, kv_dtype dtype, void* workspace,
-                                    size_t workspace_bytes, void* stream) {
+                   const int32_t* block_table, const int32_t* seq_lens,
+                   const int32_t* cu_seqlens_q, void* out, int num_seqs, int total_q_tokens,
+                   int max_num_batched_tokens, int num_q_heads, int num_kv_heads, int head_dim,
+                   int block_size, int max_blocks_per_seq, int max_seq_len, float scale,
+                   kv_dtype dtype, void* workspace, size_t workspace_bytes, void* stream) {
   if (dtype == KV_F32)
     return set_error(KV_ERR_UNSUPPORTED, "%s: fp32 prefill is not built", fn);
   if (dtype != KV_BF16)
@@ -427,23 +425,23 @@ extern "C" int kvattn_prefill_chunk(const void* q, const void* kv_layer, int num
                                     float scale, kv_dtype dtype, void* workspace,
                                     size_t workspace_bytes, void* stream) {
   clear_error();
-  return prefill_common("kvattn_prefill_chunk", false, q, kv_layer, num_blocks, block_table, seq_lens,
-                        cu_seqlens_q, out, num_seqs, total_q_tokens, max_num_batched_tokens,
+  return prefill_common("kvattn_prefill_chunk", false, q, kv_layer, num_blocks, block_table,
+                        seq_lens, cu_seqlens_q, out, num_seqs, total_q_tokens, max_num_batched_tokens,
                         num_q_heads, num_kv_heads, head_dim, block_size, max_blocks_per_seq,
                         max_seq_len, scale, dtype, workspace, workspace_bytes, stream);
 }
 
 extern "C" int kvattn_prefill_chunk_fp8(const void* q, const void* kv_layer, int num_blocks,
-                                    const int32_t* block_table, const int32_t* seq_lens,
-                                    const int32_t* cu_seqlens_q, void* out, int num_seqs,
-                                    int total_q_tokens, int max_num_batched_tokens,
-                                    int num_q_heads, int num_kv_heads, int head_dim,
-                                    int block_size, int max_blocks_per_seq, int max_seq_len,
-                                    float scale, kv_dtype dtype, void* workspace,
-                                    size_t workspace_bytes, void* stream) {
+                                        const int32_t* block_table, const int32_t* seq_lens,
+                                        const int32_t* cu_seqlens_q, void* out, int num_seqs,
+                                        int total_q_tokens, int max_num_batched_tokens,
+                                        int num_q_heads, int num_kv_heads, int head_dim,
+                                        int block_size, int max_blocks_per_seq, int max_seq_len,
+                                        float scale, kv_dtype dtype, void* workspace,
+                                        size_t workspace_bytes, void* stream) {
   clear_error();
-  return prefill_common("kvattn_prefill_chunk_fp8", true, q, kv_layer, num_blocks, block_table, seq_lens,
-                        cu_seqlens_q, out, num_seqs, total_q_tokens, max_num_batched_tokens,
+  return prefill_common("kvattn_prefill_chunk_fp8", true, q, kv_layer, num_blocks, block_table,
+                        seq_lens, cu_seqlens_q, out, num_seqs, total_q_tokens, max_num_batched_tokens,
                         num_q_heads, num_kv_heads, head_dim, block_size, max_blocks_per_seq,
                         max_seq_len, scale, dtype, workspace, workspace_bytes, stream);
 }

@@ -154,7 +154,8 @@ __device__ __forceinline__ void prefill_tile_fp8(
   auto my_block = [&](int id) __attribute__((always_inline)) { return tiles.block(max(id, 0)); };
   // This lane's 16 bytes of the K or V tile (at part) of a block.
   auto gather = [&](int id, uint32_t part) __attribute__((always_inline)) {
-    return *reinterpret_cast<const uint4*>(my_block(id) + (part + my_half * 1024) + (uint32_t)lane * 16);
+    return *reinterpret_cast<const uint4*>(my_block(id) + (part + my_half * 1024) +
+                                           (uint32_t)lane * 16);
   };
   uint4 rk, rv;   // of K of step i + 2 and V of step i, at the beginning of phase i
   // The exponents of a block, K's in the low byte.
@@ -183,7 +184,10 @@ __device__ __forceinline__ void prefill_tile_fp8(
   auto v_masked = [&](int step, int id) __attribute__((always_inline)) {
     return id < 0 || step * kKeys + (my_kb + 1) * kBS > L;
   };
-  auto v_patch = [&](int step, int id) __attribute__((always_inline)) {
+  // Codes of zero, and for a block that is not there also an exponent of its own: the
+  // byte read in its place (block 0's) may be 255, which makes NaN of any code.
+  auto v_patch = [&](int step, int id, uint32_t& exps) __attribute__((always_inline)) {
+    if (id < 0) exps = 0;
     const unsigned ln = lane_id_fresh();
     const uint32_t keep =
         id < 0 ? 0u : first_bytes(L - (step * kKeys + my_kb * kBS + (int)(ln / 16) * 4));
@@ -196,13 +200,15 @@ __device__ __forceinline__ void prefill_tile_fp8(
   };
   auto convert_v = [&](int step, int id, uint32_t exps) __attribute__((always_inline)) {
     const int buf = step % kBufs;
-    if (v_masked(step, id)) v_patch(step, id);
+    if (v_masked(step, id)) v_patch(step, id, exps);
     put_v(buf, v_at, 0, rv.x, v_scale(exps));
     put_v(buf, v_at, 1, rv.y, v_scale(exps));
     put_v(buf, v_at, 2, rv.z, v_scale(exps));
     put_v(buf, v_at, 3, rv.w, v_scale(exps));
   };
-  auto step_clean = [&](int step, int bits) __attribute__((always_inline)) { return bits == 0xf && (step + 1) * kKeys <= L; };
+  auto step_clean = [&](int step, int bits) __attribute__((always_inline)) {
+    return bits == 0xf && (step + 1) * kKeys <= L;
+  };
 
   const int wave_pos0 = c + row0;   // position of the wave's first row
   const int v_read = lm * 32 + ((lh ^ ((lm >> 3) & 1)) * 16);
@@ -289,7 +295,8 @@ __device__ __forceinline__ void prefill_tile_fp8(
   // follows them.
   // parity: i % 2, in the loop a constant, so that the buffers' addresses are too.
   auto phase = [&](auto qk_tag, auto pv_tag, auto parity, int i, f32x16_t (&s_cur)[2],
-                   f32x16_t (&s_nxt)[2], const bf16x8_t (&p_prev)[4], bf16x8_t (&p_cur)[4]) __attribute__((always_inline)) {
+                   f32x16_t (&s_nxt)[2], const bf16x8_t (&p_prev)[4],
+                   bf16x8_t (&p_cur)[4]) __attribute__((always_inline)) {
     constexpr bool kQK = decltype(qk_tag)::value;
     constexpr bool kPV = decltype(pv_tag)::value;
     const int cur = parity, nxt = 1 - cur;   // buffers of steps i and i + 1
@@ -301,7 +308,7 @@ __device__ __forceinline__ void prefill_tile_fp8(
     __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
     if (needs_mask(i, bits & 0xf)) mask_scores(i, bits & 0xf, s_cur);
     // here and not where it is converted, so that no branch splits the slots
-    if (v_masked(i, v_id)) v_patch(i, v_id);
+    if (v_masked(i, v_id)) v_patch(i, v_id, v_exps);
 
     const int vbuf = nxt;   // V of step i - 1
     const int kbuf = nxt;   // K of step i + 1

@@ -194,6 +194,36 @@ def test_bad_ids_contribute_nothing(decode):
         assert_close(got[r0:r0 + n].numpy(), ref.numpy(), w.numpy(), f"bad ids {s}")
 
 
+@pytest.mark.parametrize("decode", [True, False])
+@pytest.mark.parametrize("byte", [0, 127, 255])
+def test_blocks_that_nobody_wrote(decode, byte):
+    """What never-written blocks hold (block 0 among them), exponents outside 10 .. 246 too,
+    does not reach an output: sequences that end inside a step, and entries of -1."""
+    lens = [1, 17, 40, 300, 70]
+    new = [1] * 5 if decode else [1, 17, 33, 100, 2]
+    b, raw = fp8_batch(lens, new, hq=8, hkv=2, d=128, seed=31)
+    bb = fp8.block_bytes(2, 128)
+    at = 2 * 2 * 16 * 128
+    lay = np.concatenate([np.full((1, bb), byte, np.uint8), raw.reshape(-1, bb)])
+    free = np.setdiff1d(np.arange(b.num_blocks), b.block_table[b.block_table >= 0])
+    lay[1 + free] = byte
+    lay[:, at + 4:] = byte                               # the padding
+    dev, clean = Dev8(b, lay.reshape(-1)), Dev8(b, raw)
+    bt = b.block_table.copy()
+    bt[3, 4] = -1
+    clean.bt = torch.from_numpy(bt).cuda()
+    dev.bt = torch.from_numpy(np.where(bt >= 0, bt + 1, -1).astype(np.int32)).cuda()
+    say("fp8 unwritten blocks", decode, byte)
+    small = K.workspace(-(-(8 * (sum(new) // 32 + 6) + 16) // 256) * 256)
+    b.num_blocks += 1
+    got = [dev.decode()] if decode else [dev.prefill(), dev.prefill(ws=small)]
+    b.num_blocks -= 1
+    want = [clean.decode()] if decode else [clean.prefill(), clean.prefill(ws=small)]
+    for x, y in zip(got, want):
+        assert torch.isfinite(x.float()).all()
+        assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+
+
 def _contig(b):
     x = b.kv_layer.double().view(b.num_blocks, 2, b.num_kv_heads, -1)
     ks, vs = [], []
