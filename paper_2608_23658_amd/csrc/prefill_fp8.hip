@@ -164,7 +164,9 @@ __device__ __forceinline__ void prefill_tile_fp8(
     return scalar_word(my_block(id) + (tiles.e_off & ~3u));
   };
   auto k_scale = [&](uint32_t w) { return fp8_scale((w >> e_shift) & 0xff); };
-  auto v_scale = [&](uint32_t w) { return fp8_scale((w >> (e_shift + 8)) & 0xff); };
+  // In place of a block that is not there block 0 is read, with codes set to zero; its byte
+  // may be 255 if nobody has written it, a scale that makes NaN of zero too: at most 254.
+  auto v_scale = [&](uint32_t w) { return fp8_scale(min((w >> (e_shift + 8)) & 0xff, 254u)); };
   // Where the lane's converted pieces go. K: 16 dims of one token are two 16-byte
   // chunks of the chunk-major tile. V: dword w is tokens 4 (lane / 16) .. + 4 of dim
   // 64 half + 16 w + lane % 16, eight bytes of its row; a row's two 16-byte halves are
@@ -184,10 +186,7 @@ __device__ __forceinline__ void prefill_tile_fp8(
   auto v_masked = [&](int step, int id) __attribute__((always_inline)) {
     return id < 0 || step * kKeys + (my_kb + 1) * kBS > L;
   };
-  // Codes of zero, and for a block that is not there also an exponent of its own: the
-  // byte read in its place (block 0's) may be 255, which makes NaN of any code.
-  auto v_patch = [&](int step, int id, uint32_t& exps) __attribute__((always_inline)) {
-    if (id < 0) exps = 0;
+  auto v_patch = [&](int step, int id) __attribute__((always_inline)) {
     const unsigned ln = lane_id_fresh();
     const uint32_t keep =
         id < 0 ? 0u : first_bytes(L - (step * kKeys + my_kb * kBS + (int)(ln / 16) * 4));
@@ -200,7 +199,7 @@ __device__ __forceinline__ void prefill_tile_fp8(
   };
   auto convert_v = [&](int step, int id, uint32_t exps) __attribute__((always_inline)) {
     const int buf = step % kBufs;
-    if (v_masked(step, id)) v_patch(step, id, exps);
+    if (v_masked(step, id)) v_patch(step, id);
     put_v(buf, v_at, 0, rv.x, v_scale(exps));
     put_v(buf, v_at, 1, rv.y, v_scale(exps));
     put_v(buf, v_at, 2, rv.z, v_scale(exps));
@@ -308,7 +307,7 @@ __device__ __forceinline__ void prefill_tile_fp8(
     __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
     if (needs_mask(i, bits & 0xf)) mask_scores(i, bits & 0xf, s_cur);
     // here and not where it is converted, so that no branch splits the slots
-    if (v_masked(i, v_id)) v_patch(i, v_id, v_exps);
+    if (v_masked(i, v_id)) v_patch(i, v_id);
 
     const int vbuf = nxt;   // V of step i - 1
     const int kbuf = nxt;   // K of step i + 1
