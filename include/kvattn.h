@@ -277,7 +277,9 @@ int kvattn_kv_append(const void* k_new, const void* v_new, const int32_t* slot_m
  * products are of bf16 (codes times their power of two are exact there), sums and
  * softmax in fp32; the prefill's scale must be above zero, and its total_q_tokens may
  * exceed cu_seqlens_q[num_seqs] (a padded step): rows behind the last sequence's are
- * left as they are. Supported: decode head_dim 64 and 128, prefill 128; block_size
+ * left as they are. A NaN in the cache reaches outputs of its own sequence alone: those of
+ * the rows that see the token and, from V, maybe those of earlier rows of the same chunk
+ * (their weight for it is zero, and zero times NaN is NaN). Supported: decode head_dim 64 and 128, prefill 128; block_size
  * 16; num_q_heads / num_kv_heads in {1, 2, 4, 8}. */
 size_t kvattn_fp8_block_bytes(int num_kv_heads, int head_dim);
 

@@ -224,6 +224,32 @@ def test_blocks_that_nobody_wrote(decode, byte):
         assert torch.equal(x.view(torch.int16), y.view(torch.int16))
 
 
+@pytest.mark.parametrize("decode", [True, False])
+def test_nan_stays_in_its_sequence(decode):
+    """NaN in q, in K and in V of some sequences: the others' bits do not change, a row that sees
+    one is NaN, and a NaN in K of a chunk's last token leaves the earlier rows alone."""
+    lens = [300, 41, 130, 1100, 16]
+    new = [1] * 5 if decode else [100, 41, 7, 1, 16]
+    b, raw = fp8_batch(lens, new, hq=8, hkv=2, d=128, seed=77)
+    clean = Dev8(b, raw)
+    lay = fp8.Layer(raw.copy(), 2, 128)
+    blk = int(b.block_table[0, 299 // 16])
+    lay.tile(blk, 0, 0)[fp8.place(0, 299 % 16, 5)] = 0x7F     # K of the last token of 0, head 0
+    blk = int(b.block_table[2, 3])
+    lay.tile(blk, 1, 1)[fp8.place(1, 2, 64)] = 0xFF           # V of token 50 of 2, head 1
+    dev = Dev8(b, lay.raw.reshape(-1))
+    dev.q[-1, 3] = float("nan")                               # the last row of 4, one head
+    say("fp8 nan", decode)
+    x, y = (d.decode() if decode else d.prefill() for d in (dev, clean))
+    want = torch.zeros(x.shape, dtype=torch.bool, device="cuda")
+    at = [int(i) for i in b.cu_seqlens_q]
+    want[at[1] - 1, :4] = True
+    want[at[2]:at[3], 4:, 64] = True
+    want[-1, 3] = True
+    assert torch.equal(torch.isnan(x.float()), want)
+    assert torch.equal(x.view(torch.int16)[~want], y.view(torch.int16)[~want])
+
+
 def _contig(b):
     x = b.kv_layer.double().view(b.num_blocks, 2, b.num_kv_heads, -1)
     ks, vs = [], []
