@@ -171,6 +171,24 @@ def _stream(stream) -> int:
     return stream.cuda_stream
 
 
+def _made_for(stream, make, *args, returned=False):
+    """``make(*args)``, the tensors a call makes, for the stream it was given (None: the
+    current one). Memory that the allocator hands out again may still be used by work
+    pending on the stream it was made for, which only that stream's launches wait for, so
+    that stream has to be the call's. What the caller gets (``returned``) is used
+    on the current stream as well, and must not be handed out again before that is done."""
+    if stream is None:
+        return make(*args)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
+        made = make(*args)
+    if returned:
+        for t in made if isinstance(made, tuple) else (made,):
+            t.record_stream(torch.cuda.current_stream(t.device))
+    return made
+
+
 def _require_cuda(*ts):
     """Tensors reach the library as bare pointers, so they must be contiguous
     (checked first, which also runs without a GPU) and on the GPU."""
@@ -381,17 +399,6 @@ def _require_here(*ts):
                                  f"not {t.device}")
 
 
-def _for_stream(stream, *ts):
-    """Tensors made here that a call uses on a stream of the caller's choice: the
-    allocator must not hand them out again before that stream is done."""
-    if stream is None:
-        return
-    if isinstance(stream, int):
-        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
-    for t in ts:
-        t.record_stream(stream)
-
-
 def fp8_block_bytes(num_kv_heads: int, head_dim: int) -> int:
     """Bytes of one block of a layer in 8 bits (also copy_blocks' block_bytes)."""
     return int(lib().kvattn_fp8_block_bytes(num_kv_heads, head_dim))
@@ -436,11 +443,9 @@ def decode_fp8(q: torch.Tensor, kv_layer, num_blocks: int, block_table: torch.Te
     _require_fp8_layer(kv_layer, num_blocks, num_kv_heads, d)
     _require_here(q, kv_layer, block_table, seq_lens, out, ws)
     if out is None:
-        out = torch.empty_like(q)
-        _for_stream(stream, out)
+        out = _made_for(stream, torch.empty_like, q, returned=True)
     if ws is None:
-        ws = workspace(decode_workspace_bytes(B, Hq, d, max_seq_len), q.device)
-        _for_stream(stream, ws)
+        ws = _made_for(stream, workspace, decode_workspace_bytes(B, Hq, d, max_seq_len), q.device)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     check(lib().kvattn_decode_fp8(q.data_ptr(), _ptr(kv_layer), int(num_blocks),
                                   block_table.data_ptr(), seq_lens.data_ptr(), out.data_ptr(), B,
@@ -466,11 +471,9 @@ def prefill_chunk_fp8(q: torch.Tensor, kv_layer, num_blocks: int, block_table: t
     _require_fp8_layer(kv_layer, num_blocks, num_kv_heads, d)
     _require_here(q, kv_layer, block_table, seq_lens, cu_seqlens_q, out, ws)
     if out is None:
-        out = torch.empty_like(q)
-        _for_stream(stream, out)
+        out = _made_for(stream, torch.empty_like, q, returned=True)
     if ws is None:
-        ws = workspace(prefill_workspace_bytes(B, T, Hq, d), q.device)
-        _for_stream(stream, ws)
+        ws = _made_for(stream, workspace, prefill_workspace_bytes(B, T, Hq, d), q.device)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     budget = T if max_num_batched_tokens is None else int(max_num_batched_tokens)
     check(lib().kvattn_prefill_chunk_fp8(q.data_ptr(), _ptr(kv_layer), int(num_blocks),
@@ -519,8 +522,7 @@ def step_map(cached_lens: torch.Tensor, new_lens: torch.Tensor, free_ids: torch.
         raise ValueError(f"block_table must have {S} rows, not {block_table.shape[0]}")
     if out is None:
         _require_here(cached_lens, new_lens, free_ids, block_table)
-        out = StepMap.empty(S, max_tokens, block_table.device)
-        _for_stream(stream, *out)
+        out = _made_for(stream, StepMap.empty, S, max_tokens, block_table.device, returned=True)
     else:
         want = (S, S + 1, max_tokens, max_tokens, 2)
         if any(t.dtype != i32 or tuple(t.shape) != (n,) for t, n in zip(out, want)):
