@@ -261,9 +261,9 @@ def decode_two_tensor(q: torch.Tensor, kv_base, num_base: int, kv_elastic, num_e
     _require_out(out, q)
     _require_cuda(q, kv_base, kv_elastic, block_table, seq_lens, out, ws)
     if out is None:
-        out = torch.empty_like(q)
+        out = _made_for(stream, torch.empty_like, q, returned=True)
     if ws is None:
-        ws = workspace(decode_workspace_bytes(B, Hq, d, max_seq_len), q.device)
+        ws = _made_for(stream, workspace, decode_workspace_bytes(B, Hq, d, max_seq_len), q.device)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     rc = lib().kvattn_decode_two_tensor(q.data_ptr(), _ptr(kv_base), int(num_base),
                                         _ptr(kv_elastic), int(num_elastic), block_table.data_ptr(),
@@ -301,9 +301,9 @@ def decode(q: torch.Tensor, kv_layer, num_blocks: int, block_table: torch.Tensor
     _require_out(out, q)
     _require_cuda(q, kv_layer, block_table, seq_lens, out, ws)
     if out is None:
-        out = torch.empty_like(q)
+        out = _made_for(stream, torch.empty_like, q, returned=True)
     if ws is None:
-        ws = workspace(decode_workspace_bytes(B, Hq, d, max_seq_len), q.device)
+        ws = _made_for(stream, workspace, decode_workspace_bytes(B, Hq, d, max_seq_len), q.device)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     rc = lib().kvattn_decode(q.data_ptr(), _ptr(kv_layer), int(num_blocks), block_table.data_ptr(),
                              seq_lens.data_ptr(), out.data_ptr(), B, Hq, int(num_kv_heads), d,
@@ -354,9 +354,9 @@ def prefill_chunk(q: torch.Tensor, kv_layer, num_blocks: int, block_table: torch
     _require_out(out, q)
     _require_cuda(q, kv_layer, block_table, seq_lens, cu_seqlens_q, out, ws)
     if out is None:
-        out = torch.empty_like(q)
+        out = _made_for(stream, torch.empty_like, q, returned=True)
     if ws is None:
-        ws = workspace(prefill_workspace_bytes(B, T, Hq, d), q.device)
+        ws = _made_for(stream, workspace, prefill_workspace_bytes(B, T, Hq, d), q.device)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     budget = T if max_num_batched_tokens is None else int(max_num_batched_tokens)
     rc = lib().kvattn_prefill_chunk(q.data_ptr(), _ptr(kv_layer), int(num_blocks),
@@ -832,7 +832,8 @@ def probe_mfma(num_workgroups: int, iters: int, out: Optional[torch.Tensor] = No
     its shader-clock and real-time counters around its loop."""
     n = num_workgroups * int(lib().kvattn_probe_mfma_threads())
     if out is None:
-        out = torch.empty(n, dtype=torch.float32, device="cuda")
+        out = _made_for(stream, lambda: torch.empty(n, dtype=torch.float32, device="cuda"),
+                        returned=True)
     if out.dtype != torch.float32 or out.numel() < n:
         raise ValueError(f"out must hold {n} float32")
     if clocks is not None and (clocks.dtype != torch.int64 or
@@ -880,7 +881,8 @@ def probe_read_blocks(kv_layer, num_blocks: int, block_table: torch.Tensor,
     if waves <= 0:
         raise ValueError("invalid or too large batch for the read probe")
     if out is None:
-        out = torch.empty(waves * 64, dtype=torch.int32, device="cuda")
+        out = _made_for(stream, lambda: torch.empty(waves * 64, dtype=torch.int32, device="cuda"),
+                        returned=True)
     if out.dtype != torch.int32 or out.numel() < waves * 64:
         raise ValueError(f"out must hold {waves * 64} int32")
     _require_cuda(kv_layer, block_table, seq_lens, out)

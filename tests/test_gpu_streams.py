@@ -5,7 +5,8 @@ import torch
 
 import paper_2608_23658_amd.kvattn as K
 from tests.fp8_helpers import Dev8, fp8_batch
-from tests.gpu_helpers import require_gpu, say
+from tests.gpu_helpers import Dev, require_gpu, say
+from workloads import make_batch_from_lens
 
 pytestmark = pytest.mark.gpu
 HQ, HKV, D = 8, 2, 128
@@ -36,7 +37,18 @@ def _step_map():
     return lambda **kw: list(K.step_map(cached, new, free, table, max_tokens=1000, **kw)), []
 
 
-CALLS = {"decode_fp8": _decode_fp8, "prefill_chunk_fp8": _prefill_chunk_fp8,
+def _bf16(decode):
+    b = make_batch_from_lens([3000, 900, 1500, 1] if decode else [700, 300],
+                             [1] * 4 if decode else [200, 300], dtype="bf16", num_q_heads=HQ,
+                             num_kv_heads=HKV, head_dim=D, block_size=16, seed=53)
+    x = Dev(b)
+    ws = (K.decode_workspace_bytes(4, HQ, D, 3000) if decode else
+          K.prefill_workspace_bytes(2, 500, HQ, D))
+    return lambda **kw: [(x.decode if decode else x.prefill)(**kw)], [ws]
+
+
+CALLS = {"decode": lambda: _bf16(True), "prefill_chunk": lambda: _bf16(False),
+         "decode_fp8": _decode_fp8, "prefill_chunk_fp8": _prefill_chunk_fp8,
          "step_map": _step_map}
 
 

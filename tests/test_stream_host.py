@@ -18,10 +18,11 @@ HERE, OTHER = Stream(0x1000), Stream(0x2000)
 
 
 class Library:
-    """Every call succeeds; sizes are a page."""
+    """Every call succeeds; sizes are a page, counts 64."""
 
     def __getattr__(self, name):
-        return lambda *a: 4096 if name.endswith("bytes") else K.KV_OK
+        return lambda *a: (4096 if name.endswith("bytes") else
+                           64 if name.endswith(("threads", "waves")) else K.KV_OK)
 
 
 class Notes:
@@ -43,7 +44,7 @@ def notes(monkeypatch):
 
     def noting(make):
         def made(*a, **kw):
-            t = make(*a, **kw)
+            t = make(*a, **dict(kw, device="cpu") if "device" in kw else kw)
             n.made.append((t.data_ptr(), n.on.cuda_stream))
             return t
         return made
@@ -75,6 +76,13 @@ KW = dict(num_kv_heads=2, max_seq_len=48)
 CALLS = {
     "decode_fp8": lambda **kw: K.decode_fp8(*_batch(), **KW, **kw),
     "prefill_chunk_fp8": lambda **kw: K.prefill_chunk_fp8(*_batch(), _i32(5), **KW, **kw),
+    "decode": lambda **kw: K.decode(*_batch(), **KW, **kw),
+    "decode_two_tensor": lambda **kw: K.decode_two_tensor(
+        _batch()[0], _batch()[1], 1, _batch()[1], 1, *_batch()[3:], **KW, **kw),
+    "prefill_chunk": lambda **kw: K.prefill_chunk(*_batch(), _i32(5), **KW, **kw),
+    "probe_mfma": lambda **kw: K.probe_mfma(1, 1, **kw),
+    "probe_read_blocks": lambda **kw: K.probe_read_blocks(
+        *_batch()[1:], head_dim=128, dtype=torch.bfloat16, **KW, **kw),
     "step_map": lambda **kw: K.step_map(_i32(4), _i32(4), _i32(5), _i32(4, 3), max_tokens=10,
                                         **kw),
 }
