@@ -275,7 +275,8 @@ int kvattn_kv_append(const void* k_new, const void* v_new, const int32_t* slot_m
  * kvattn_prefill_chunk over such a layer: same arguments, workspaces (of the same
  * size functions) and rules; dtype is the type of q and out and must be KV_BF16. The
  * products are of bf16 (codes times their power of two are exact there), sums and
- * softmax in fp32; the prefill's scale must be above zero, and its total_q_tokens may
+ * softmax in fp32; scale * log2(e) must be finite (KV_ERR_INVALID), and the prefill's
+ * scale above zero; the prefill's total_q_tokens may
  * exceed cu_seqlens_q[num_seqs] (a padded step): rows behind the last sequence's are
  * left as they are. A NaN in the cache reaches outputs of its own sequence alone: those of
  * the rows that see the token and, from V, maybe those of earlier rows of the same chunk

@@ -151,6 +151,9 @@ extern "C" size_t kvattn_decode_workspace_bytes(int num_seqs, int num_q_heads, i
 }
 
 namespace {
+// The kernels take softmax in powers of two: an infinite scale * log2(e) would make NaN of
+// a score of zero.
+bool scale_log2_ok(float scale) { return std::isfinite(scale * kvattn::kLog2e); }
 
 // Checks a decode call and fills the launch descriptor; the workspace is
 // checked only when check_workspace is set.
@@ -270,6 +273,8 @@ int decode_check(const char* fn, const void* q, const void* kv_layer, const void
                      max_seq_len, max_blocks_per_seq, block_size);
   if (num_blocks <= 0) return set_error(KV_ERR_INVALID, "%s: num_blocks %d", fn, num_blocks);
   if (!std::isfinite(scale)) return set_error(KV_ERR_INVALID, "%s: scale not finite", fn);
+  if (fp8 && !scale_log2_ok(scale))
+    return set_error(KV_ERR_INVALID, "%s: scale %g is too large", fn, scale);
   if (num_kv_heads > 65535 || num_seqs > 65535)
     return set_error(KV_ERR_UNSUPPORTED, "%s: grid too large", fn);
   if (num_seqs == 0) return KV_OK;
@@ -375,6 +380,8 @@ int prefill_common(const char* fn, bool fp8, const void* q, const void* kv_layer
     return set_error(KV_ERR_INVALID, "%s: num_blocks %d", fn, num_blocks);
   if (!std::isfinite(scale))
     return set_error(KV_ERR_INVALID, "%s: scale not finite", fn);
+  if (fp8 && !scale_log2_ok(scale))
+    return set_error(KV_ERR_INVALID, "%s: scale %g is too large", fn, scale);
   // masked scores are minus infinity before the scale
   if (fp8 && !(scale > 0.f))
     return set_error(KV_ERR_INVALID, "%s: scale %g must be above zero", fn, scale);

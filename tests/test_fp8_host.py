@@ -65,6 +65,16 @@ def test_prefill_refuses(L, kw, code):
     assert K.last_error().startswith("kvattn_prefill_chunk_fp8")
 
 
+@pytest.mark.parametrize("scale", [3e38, 2.4e38])
+def test_scales_past_log2(L, scale):
+    """The kernels work in powers of two, with scale * log2(e): infinite, it would make NaN of
+    every score of zero."""
+    for call, name in ((_decode, "kvattn_decode_fp8"), (_prefill, "kvattn_prefill_chunk_fp8")):
+        assert call(L, scale=scale) == K.KV_ERR_INVALID
+        assert K.last_error().startswith(name) and "scale" in K.last_error()
+    assert _decode(L, scale=-scale) == K.KV_ERR_INVALID
+
+
 def _append(L, **kw):
     a = dict(k=A, v=A, sm=A, kv=A, nb=100, T=64, hkv=8, d=128, bs=16, dt=K.KV_BF16)
     a.update(kw)
