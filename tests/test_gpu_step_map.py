@@ -151,3 +151,19 @@ def test_captured_steps_replayed():
         assert out.slot_mapping.tolist() == slots and out.positions.tolist() == pos
         assert np.array_equal(table.cpu().numpy(), want)
         (torch.ones(1000, device="cuda") * 2).sum().item()   # the program's own work between
+
+
+@pytest.mark.parametrize("S,MB,hi,T", [
+    (4097, 5, 9, 3000),    # the budget ends in the first of three tiles of requests
+    (4097, 5, 9, 7000),    # in the second
+    (9001, 3, 6, 5000),    # tiles behind it are granted nothing
+    (9001, 3, 6, 17000),   # in the last
+    (2049, 5, 9, 0), (2049, 5, 9, 1),
+])
+def test_budgets_that_end_inside_a_later_tile(S, MB, hi, T):
+    cached, new, free, table = _random(S + T, S, MB, hi)
+    room = np.minimum(new, MB * 16 - cached)
+    assert room.sum() > T
+    say("step map: budget", S, MB, hi, T, "of", int(room.sum()))
+    _check(cached, new, free, table, T)
+    _check(cached, new, free[:T // 64], table, T)      # and too few ids
