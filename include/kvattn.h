@@ -263,7 +263,8 @@ int kvattn_kv_append(const void* k_new, const void* v_new, const int32_t* slot_m
  * exponent is e (what other slots held has no meaning any more); any other call
  * takes max(e, the block's exponent), and where that is larger the block's other codes
  * are rounded to the new scale (exact but for those that leave e4m3's normal range, below
- * 2^-14 of the largest value). Values are rounded to nearest even; NaN and
+ * 2^-6 of the new power of two, which is under 2^-13.8 of the largest new value).
+ * Values are rounded to nearest even; NaN and
  * infinities become NaN, finite values beyond 448 * 2^119 the largest code. Skipped
  * slots and alignment as for kvattn_kv_append. A block with a repeated slot, or whose
  * tokens stand in several places of one call's list (a skipped slot between them

@@ -95,3 +95,24 @@ def test_step_map_by_hand():
     assert slots[:3] == [8 * 16 + 1, 48, 49] and slots[17:20] == [64, 65, 80]
     assert pos[0] == 17 and pos[19] == 16
     assert out.tolist() == [[7, 8, -1, -1], [3, 4, -1, -1], [9, 5, -1, -1]]
+
+
+def test_scaling_anew_is_exact_down_to_the_normal_range():
+    """A block's code c 2^old under the exponent of larger values: exact where it is at least
+    2^-6 of the new power of two, which is less than 2^-13.8 of the largest, and not 2^-14 of
+    it: 225 takes exponent 0, and 2^-13.9 of that is rounded."""
+    codes = fp8.decode(np.arange(127, dtype=np.uint8))
+    for amax in (225.0, 300.0, 448.0, 449.0, 1e5):
+        e = int(fp8.exponent(amax))
+        assert 2.0 ** (e - 6) < 2.0 ** -13.8 * amax
+        for old in range(e - 24, e):
+            v = codes * 2.0 ** old
+            got = fp8.decode(fp8.encode(v * 2.0 ** -e)) * 2.0 ** e
+            normal = v >= 2.0 ** (e - 6)
+            assert np.array_equal(got[normal], v[normal])
+    raw = np.zeros(fp8.block_bytes(1, 64), np.uint8)
+    small, large = np.full((1, 1, 64), 0.0146484375), np.full((1, 1, 64), 225.0)
+    assert 2.0 ** -14 < 0.0146484375 / 225 < 2.0 ** -13.8
+    for slot, x, seen in ((0, small, 0.0146484375), (1, large, 0.015625)):
+        raw = fp8.append(raw, x, x, [slot], num_kv_heads=1, head_dim=64)
+        assert (fp8.Layer(raw, 1, 64).values(0, 0, 0)[0] == seen).all()
