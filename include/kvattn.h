@@ -275,14 +275,16 @@ int kvattn_kv_append(const void* k_new, const void* v_new, const int32_t* slot_m
  * kvattn_decode_fp8, kvattn_prefill_chunk_fp8: kvattn_decode and
  * kvattn_prefill_chunk over such a layer: same arguments, workspaces (of the same
  * size functions) and rules; dtype is the type of q and out and must be KV_BF16. The
- * products are of bf16 (codes times their power of two are exact there), sums and
- * softmax in fp32; scale * log2(e) must be finite (KV_ERR_INVALID), and the prefill's
- * scale above zero; the prefill's total_q_tokens may
- * exceed cu_seqlens_q[num_seqs] (a padded step): rows behind the last sequence's are
- * left as they are. A NaN in the cache reaches outputs of its own sequence alone: those of
- * the rows that see the token and, from V, maybe those of earlier rows of the same chunk
- * (their weight for it is zero, and zero times NaN is NaN). Supported: decode head_dim 64 and 128, prefill 128; block_size
- * 16; num_q_heads / num_kv_heads in {1, 2, 4, 8}. */
+ * products are of bf16 and their sums of fp32. Codes times their power of two are exact in
+ * bf16. Softmax is in fp32, and each weight is rounded to bf16 (by at most 2^-8 of itself)
+ * before it multiplies V and before it joins the row sum, as over a bf16 layer; the output
+ * is rounded once. scale * log2(e) must be finite, and the prefill's scale above zero
+ * (KV_ERR_INVALID). The prefill's total_q_tokens may exceed cu_seqlens_q[num_seqs] (a
+ * padded step): rows behind the last sequence's are left as they are. A NaN in the cache
+ * reaches outputs of its own sequence alone: those of the rows that see the token and, from
+ * V, maybe those of earlier rows of the same chunk (their weight for it is zero, and zero
+ * times NaN is NaN). Supported: decode head_dim 64 and 128, prefill 128; block_size 16;
+ * num_q_heads / num_kv_heads in {1, 2, 4, 8}. */
 size_t kvattn_fp8_block_bytes(int num_kv_heads, int head_dim);
 
 int kvattn_kv_append_fp8(const void* k_new, const void* v_new, const int32_t* slot_mapping,

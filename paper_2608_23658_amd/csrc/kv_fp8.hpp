@@ -170,7 +170,9 @@ __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* 
     for (int j = 0; j < kTB; ++j) {
       pw[j].x = pack_bf16x2(fast_exp2(x[j][0] - ref), fast_exp2(x[j][1] - ref));
       pw[j].y = pack_bf16x2(fast_exp2(x[j][2] - ref), fast_exp2(x[j][3] - ref));
-      // the row sum adds the bf16 values that p.v multiplies
+      // A weight is rounded to bf16, as the matrix instruction takes it: at most 2^-8 of
+      // it, the size of the output's own rounding, and independent from token to
+      // token. The row sum adds the rounded weights, so that they still add up to one.
       psum = dot2_bf16(pw[j].x, kBf16OnePair, psum);
       psum = dot2_bf16(pw[j].y, kBf16OnePair, psum);
     }

@@ -354,7 +354,8 @@ __device__ __forceinline__ void prefill_tile_fp8(
         const int e = k;
         pe[e] = fast_exp2(fmaf(s_cur[e / 16][e % 16], scale_log2, -ref));
         if (e % 2 == 1) {
-          // the row sum adds the bf16 values that p.v multiplies
+          // A weight is rounded to bf16, as the matrix instruction takes it (at most 2^-8
+          // of it); the row sum adds the rounded ones, so that they add up to one.
           pw[e / 2] = pack_bf16x2(pe[e - 1], pe[e]);
           psum = dot2_bf16(pw[e / 2], kBf16OnePair, psum);
         }
