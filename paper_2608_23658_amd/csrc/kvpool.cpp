@@ -44,7 +44,7 @@ struct kvpool {
   std::vector<hipMemGenericAllocationHandle_t> whole_h;
   bool committed = false;
   bool whole = false;
-  kvpool_steps last;   // host wall time of each step of the last commit / decommit
+  kvpool_steps last = {};   // host wall time of each step of the last commit / decommit
 };
 
 namespace {

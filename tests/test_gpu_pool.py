@@ -1,6 +1,8 @@
 """The elastic per-layer pool: lifecycle, kernels over base + elastic ids,
 bit-identical results across a decommit/recommit cycle, commit failure under
 memory pressure, and decommit with work still in flight."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -193,5 +195,29 @@ def test_whole_handle_commit_decodes_and_keeps_base_bit_for_bit():
         pool.decommit()
         base = pool.layer_view(0, committed_part=False, dtype=torch.bfloat16)
         assert torch.equal(base.view(torch.int16), kv[:n_base].view(torch.int16))
+    finally:
+        pool.close()
+
+
+def test_steps_of_a_pool_that_has_not_toggled_read_zero():
+    """A step that no commit or decommit has taken yet reads 0, also where the pool's host
+    memory was used before."""
+    libc = ctypes.CDLL(None)
+    libc.malloc.restype, libc.malloc.argtypes = ctypes.c_void_p, [ctypes.c_size_t]
+    libc.free.argtypes = [ctypes.c_void_p]
+    used = [(libc.malloc(n), n) for n in range(64, 769, 8) for _ in range(4)]
+    for at, n in used:
+        ctypes.memset(at, 0x6B, n)
+    for at, _ in used:
+        libc.free(at)
+    gran = K.ElasticPool.granularity()
+    pool = K.ElasticPool(1, gran, gran)
+    say("pool steps")
+    try:
+        assert set(pool.last_steps().values()) == {0.0}
+        pool.commit()
+        steps = pool.last_steps()
+        assert all(v == 0.0 for n, v in steps.items() if n.startswith("decommit"))
+        assert steps["commit_create_ms"] > 0.0 and steps["commit_copy_ms"] == 0.0
     finally:
         pool.close()
