@@ -173,6 +173,8 @@ const char* kvattn_trace_kernel_name(int i);
  * max_num_batched_tokens  the step's token budget: total_q_tokens must not
  *               exceed it (KV_ERR_INVALID otherwise); it sizes no buffer and
  *               never changes the arithmetic
+ * scale         as for decode, above zero: masked scores are minus infinity
+ *               before it multiplies them
  * workspace     device scratch of kvattn_prefill_workspace_bytes(...) bytes, no
  *               initial contents needed, not used by another call in flight.
  *               About 65 MiB of it, whatever the sizes, hold partial results
