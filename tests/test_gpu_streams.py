@@ -105,3 +105,34 @@ def test_results_the_current_stream_still_reads(name):
         for a, b in zip(kept, want):
             assert torch.equal(a, b)
         del junk, kept
+
+
+@pytest.mark.parametrize("how", ["stream", "handle", "joined"])
+@pytest.mark.parametrize("name", ["decode_fp8", "prefill_chunk_fp8", "decode", "prefill_chunk"])
+def test_captured_with_a_stream_named(name, how):
+    """Tensors made within a capture, for the capturing stream by name or by handle, or for
+    another that joins it: the graph's own, whatever is made and dropped between replays."""
+    call, sizes = CALLS[name]()
+    want = [t.clone() for t in call()]
+    sizes = sizes + [_bytes(t) for t in want]
+    main, other = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    say("captured", name, how)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=main):
+        if how == "joined":
+            other.wait_stream(main)
+            got = call(stream=other)
+            main.wait_stream(other)
+        else:
+            got = call(stream=main if how == "stream" else main.cuda_stream)
+    for _ in range(4):
+        for t in got:
+            t.fill_(3)
+        torch.cuda.synchronize()
+        g.replay()
+        junk = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+        del junk
