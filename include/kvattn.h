@@ -309,6 +309,55 @@ int kvattn_prefill_chunk_fp8(const void* q, const void* kv_layer, int num_blocks
                              void* stream);
 
 /* ------------------------------------------------------------------------- */
+/* Between a layer's projection and its attention, in one launch: the norm of each q and
+ * k head, their rotation by position, and the new K and V written into their paged slots
+ * as kvattn_kv_append writes them.
+ *
+ * A head's row x of head_dim values:
+ *   norm      x * rsqrt(mean(x^2) + eps) * weight, if there is a weight
+ *   rotation  of the first rot_dim values, as rot_dim / 2 pairs: pair i is values
+ *             (i, i + rot_dim / 2), or (2 i, 2 i + 1) if interleaved, and becomes
+ *             (a c - b s, b c + a s) with c and s of the row of rope_table that the token's
+ *             position names; values from rot_dim on stay
+ * q and k are computed in fp32 and rounded once (mean(x^2) has fp32's range: rows of values
+ * past 2^60 are out of it); v is stored as it is.
+ *
+ * Several axes (an image's or a video's tokens: time, height, width): the first
+ * sections[0] pairs turn by positions[0], the next sections[1] by positions[1], and so on. */
+#define KVATTN_MAX_AXES 4
+typedef struct {
+  const void* q_weight;      /* device, [head_dim] of dtype, 16-B aligned; NULL: no norm of q */
+  const void* k_weight;      /* the same for k */
+  float eps;                 /* >= 0 */
+  const float* rope_table;   /* device, [rope_len][rot_dim], 16-B aligned: a position's rot_dim / 2
+                                cosines, then its sines; NULL: no rotation, and the rest unused */
+  int rope_len;              /* positions of the table; one outside it gives NaN */
+  int rot_dim;               /* 32, 64 or 128, at most head_dim */
+  int interleaved;           /* 0: pairs are half of rot_dim apart; else adjacent */
+  const int32_t* positions;  /* device, [num_axes][num_tokens] */
+  int num_axes;              /* 1 .. KVATTN_MAX_AXES */
+  int sections[KVATTN_MAX_AXES];   /* pairs of each axis, >= 0, rot_dim / 2 in all */
+} kvattn_norm_rope;
+
+/* q, k, v       device, [num_tokens][heads][head_dim] of dtype, 16-B aligned, a token's heads
+ *               next to each other and q_stride (k_stride, v_stride) elements from one token
+ *               to the next, whole 16 bytes: parts of one fused projection's output, say
+ * prep          host, read before the call returns
+ * slot_mapping  device int32 [num_tokens], as for kvattn_kv_append; the q row of a skipped
+ *               token is written all the same
+ * q_out         device, [num_tokens][num_q_heads][head_dim] of dtype, 16-B aligned. It may be q
+ *               itself where q is laid out like that; it and the layer must not overlap anything
+ *               else (KV_ERR_INVALID)
+ * kv_layer      device, one layer of dtype in the layout above, 16-B aligned
+ * Supported: bf16 and fp32, head_dim 64 and 128, block_size 16, at most 65535 heads in all.
+ * Asynchronous on stream, one launch; allocates nothing; num_tokens == 0 is a no-op. */
+int kvattn_qkv_append(const void* q, size_t q_stride, const void* k, size_t k_stride,
+                      const void* v, size_t v_stride, const kvattn_norm_rope* prep,
+                      const int32_t* slot_mapping, void* q_out, void* kv_layer, int num_blocks,
+                      int num_tokens, int num_q_heads, int num_kv_heads, int head_dim,
+                      int block_size, kv_dtype dtype, void* stream);
+
+/* ------------------------------------------------------------------------- */
 /* The maps of a step on the GPU, from the requests' lengths: what append, decode and
  * prefill read, for layers of either format (Section 1: max_num_batched_tokens
  * bounds the new tokens of one step; Section 2: blocks of fixed size are handed

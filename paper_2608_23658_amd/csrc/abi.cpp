@@ -547,6 +547,137 @@ bool overlap(const Range& a, const Range& b) {
 }
 }  // namespace
 
+namespace {
+// Checks a qkv append call and fills the launch descriptor.
+int qkv_check(const char* fn, const void* q, size_t q_stride, const void* k, size_t k_stride,
+              const void* v, size_t v_stride, const kvattn_norm_rope* prep,
+              const int32_t* slot_mapping, void* q_out, void* kv_layer, int num_blocks,
+              int num_tokens, int num_q_heads, int num_kv_heads, int head_dim, int block_size,
+              kv_dtype dtype, bool fp8, void* stream, kvattn::QkvArgs* out_args) {
+  if (dtype != KV_F32 && dtype != KV_BF16)
+    return set_error(KV_ERR_INVALID, "%s: unknown dtype %d", fn, (int)dtype);
+  const size_t esz = dtype == KV_BF16 ? 2 : 4;
+  if (num_tokens < 0) return set_error(KV_ERR_INVALID, "%s: num_tokens < 0", fn);
+  if (num_q_heads <= 0 || num_kv_heads <= 0 || head_dim <= 0)
+    return set_error(KV_ERR_INVALID, "%s: %d query and %d kv heads of dim %d", fn, num_q_heads,
+                     num_kv_heads, head_dim);
+  if ((long long)num_q_heads + 2LL * num_kv_heads > 65535)
+    return set_error(KV_ERR_UNSUPPORTED, "%s: too many heads", fn);
+  if (head_dim != 64 && head_dim != 128)
+    return set_error(KV_ERR_UNSUPPORTED, "%s: head_dim %d not built", fn, head_dim);
+  if (block_size != 16)
+    return set_error(KV_ERR_UNSUPPORTED, "%s: block_size %d not built", fn, block_size);
+  if (num_blocks <= 0 || (long long)num_blocks * block_size > 0x7fffffffLL)
+    return set_error(KV_ERR_INVALID, "%s: num_blocks %d", fn, num_blocks);
+  if (!prep) return set_error(KV_ERR_INVALID, "%s: null prep", fn);
+  if ((prep->q_weight || prep->k_weight) && !(prep->eps >= 0.f && std::isfinite(prep->eps)))
+    return set_error(KV_ERR_INVALID, "%s: eps %g", fn, prep->eps);
+  if (!aligned16(prep->q_weight) || !aligned16(prep->k_weight))
+    return set_error(KV_ERR_INVALID, "%s: weights must be 16-byte aligned", fn);
+  kvattn::QkvArgs& a = *out_args;
+  a.axis_end[0] = a.axis_end[1] = a.axis_end[2] = 0x7fffffff;
+  if (prep->rope_table) {
+    if (!aligned16(prep->rope_table) || prep->rope_len <= 0)
+      return set_error(KV_ERR_INVALID, "%s: rope_table of %d positions must be 16-byte aligned",
+                       fn, prep->rope_len);
+    if (prep->rot_dim <= 0 || prep->rot_dim % 2 || prep->rot_dim > head_dim)
+      return set_error(KV_ERR_INVALID, "%s: rot_dim %d of head_dim %d", fn, prep->rot_dim,
+                       head_dim);
+    if (prep->rot_dim != 32 && prep->rot_dim != 64 && prep->rot_dim != 128)
+      return set_error(KV_ERR_UNSUPPORTED, "%s: rot_dim %d not built", fn, prep->rot_dim);
+    if (prep->num_axes < 1 || prep->num_axes > KVATTN_MAX_AXES)
+      return set_error(KV_ERR_INVALID, "%s: %d axes", fn, prep->num_axes);
+    long long pairs = 0;
+    for (int i = 0; i < prep->num_axes; ++i) {
+      if (prep->sections[i] < 0)
+        return set_error(KV_ERR_INVALID, "%s: section %d is negative", fn, i);
+      pairs += prep->sections[i];
+      if (i + 1 < prep->num_axes) a.axis_end[i] = (int)std::min(pairs, 0x7fffffffLL);
+    }
+    if (pairs != prep->rot_dim / 2)
+      return set_error(KV_ERR_INVALID, "%s: sections of %lld pairs, rot_dim %d has %d", fn, pairs,
+                       prep->rot_dim, prep->rot_dim / 2);
+    if (num_tokens > 0 && (!prep->positions || (reinterpret_cast<uintptr_t>(prep->positions) & 3)))
+      return set_error(KV_ERR_INVALID, "%s: positions null or not 4-byte aligned", fn);
+  }
+  if (num_tokens == 0) return KV_OK;
+  if (!q || !k || !v || !slot_mapping || !q_out || !kv_layer)
+    return set_error(KV_ERR_INVALID, "%s: null pointer argument", fn);
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) ||
+      !aligned16(kv_layer))
+    return set_error(KV_ERR_INVALID,
+                     "%s: q, k, v, q_out and kv_layer must be 16-byte aligned", fn);
+  const size_t most = (size_t)1 << 40;   // elements: products below stay in 64 bits
+  if (q_stride * esz % 16 || k_stride * esz % 16 || v_stride * esz % 16 || q_stride > most ||
+      k_stride > most || v_stride > most)
+    return set_error(KV_ERR_INVALID, "%s: strides %zu, %zu, %zu must be whole 16 bytes", fn,
+                     q_stride, k_stride, v_stride);
+  const size_t rows_q = (size_t)num_q_heads * head_dim, rows_k = (size_t)num_kv_heads * head_dim;
+  const size_t last = (size_t)num_tokens - 1;
+  const size_t block_bytes = fp8 ? kvattn::fp8_block_bytes(num_kv_heads, head_dim)
+                                 : 2 * rows_k * block_size * esz;
+  const Range in[] = {{q, (last * q_stride + rows_q) * esz},
+                      {k, (last * k_stride + rows_k) * esz},
+                      {v, (last * v_stride + rows_k) * esz},
+                      {slot_mapping, (size_t)num_tokens * 4},
+                      {prep->q_weight, prep->q_weight ? head_dim * esz : 0},
+                      {prep->k_weight, prep->k_weight ? head_dim * esz : 0},
+                      {prep->rope_table, prep->rope_table
+                                             ? (size_t)prep->rope_len * prep->rot_dim * 4 : 0},
+                      {prep->positions, prep->rope_table
+                                            ? (size_t)prep->num_axes * num_tokens * 4 : 0}};
+  const Range rows_out = {q_out, (size_t)num_tokens * rows_q * esz};
+  const Range layer = {kv_layer, (size_t)num_blocks * block_bytes};
+  const bool in_place = q == q_out && (q_stride == rows_q || num_tokens == 1);
+  bool bad = overlap(rows_out, layer);
+  for (const Range& r : in)
+    bad = bad || overlap(r, layer) || (overlap(r, rows_out) && !(in_place && &r == &in[0]));
+  if (bad)
+    return set_error(KV_ERR_INVALID, "%s: q_out or kv_layer overlaps another argument", fn);
+  a.q = static_cast<const uint8_t*>(q);
+  a.k = static_cast<const uint8_t*>(k);
+  a.v = static_cast<const uint8_t*>(v);
+  a.q_stride = q_stride * esz;
+  a.k_stride = k_stride * esz;
+  a.v_stride = v_stride * esz;
+  a.q_weight = static_cast<const uint8_t*>(prep->q_weight);
+  a.k_weight = static_cast<const uint8_t*>(prep->k_weight);
+  a.eps = prep->eps;
+  a.table = prep->rope_table;
+  a.table_len = prep->rope_len;
+  a.rot = prep->rot_dim;
+  a.interleaved = prep->interleaved != 0;
+  a.positions = prep->positions;
+  a.slot_mapping = slot_mapping;
+  a.q_out = static_cast<uint8_t*>(q_out);
+  a.kv = static_cast<uint8_t*>(kv_layer);
+  a.num_blocks = num_blocks;
+  a.num_tokens = num_tokens;
+  a.num_q_heads = num_q_heads;
+  a.num_kv_heads = num_kv_heads;
+  a.head_dim = head_dim;
+  a.esz = (int)esz;
+  a.stream = static_cast<hipStream_t>(stream);
+  return KV_OK;
+}
+}  // namespace
+
+extern "C" int kvattn_qkv_append(const void* q, size_t q_stride, const void* k, size_t k_stride,
+                                 const void* v, size_t v_stride, const kvattn_norm_rope* prep,
+                                 const int32_t* slot_mapping, void* q_out, void* kv_layer,
+                                 int num_blocks, int num_tokens, int num_q_heads,
+                                 int num_kv_heads, int head_dim, int block_size, kv_dtype dtype,
+                                 void* stream) {
+  clear_error();
+  const char* fn = "kvattn_qkv_append";
+  kvattn::QkvArgs a;
+  const int rc = qkv_check(fn, q, q_stride, k, k_stride, v, v_stride, prep, slot_mapping, q_out,
+                           kv_layer, num_blocks, num_tokens, num_q_heads, num_kv_heads, head_dim,
+                           block_size, dtype, false, stream, &a);
+  if (rc != KV_OK || num_tokens == 0) return rc;
+  return hip_status(kvattn::launch_qkv_append(a), fn);
+}
+
 extern "C" int kvattn_step_map(const int32_t* cached_lens, const int32_t* new_lens, int num_seqs,
                                const int32_t* free_ids, int num_free, int32_t* block_table,
                                int max_blocks_per_seq, int block_size, int max_tokens,

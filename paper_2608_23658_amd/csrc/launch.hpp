@@ -59,6 +59,23 @@ struct AppendArgs {
   hipStream_t stream;
 };
 
+struct QkvArgs {
+  const uint8_t *q, *k, *v;
+  size_t q_stride, k_stride, v_stride;   // bytes from token to token
+  const uint8_t *q_weight, *k_weight;    // null: rows are not normed
+  float eps;
+  const float* table;                    // null: rows are not rotated
+  int table_len, rot;
+  bool interleaved;
+  const int32_t* positions;              // [axes][num_tokens]
+  int axis_end[3];                       // first pair past axes 0, 1, 2
+  const int32_t* slot_mapping;
+  uint8_t *q_out, *kv;
+  int num_blocks, num_tokens, num_q_heads, num_kv_heads, head_dim;
+  int esz;   // bytes per element of the rows: 2 (bf16) or 4 (fp32)
+  hipStream_t stream;
+};
+
 struct StepMapArgs {
   const int32_t *cached, *wanted;
   int num_seqs;
@@ -93,6 +110,7 @@ hipError_t launch_decode(const DecodeArgs& a);
 hipError_t launch_prefill(const PrefillArgs& a);
 hipError_t launch_append(const AppendArgs& a);
 hipError_t launch_append_fp8(const AppendArgs& a);
+hipError_t launch_qkv_append(const QkvArgs& a);
 hipError_t launch_step_map(const StepMapArgs& a);
 hipError_t launch_copy_blocks(const CopyArgs& a);
 

@@ -39,6 +39,15 @@ class KvPoolSteps(ctypes.Structure):
     _fields_ = [(n, ctypes.c_double) for n in POOL_STEPS]
 
 
+class NormRope(ctypes.Structure):
+    """``kvattn_norm_rope``: how a qkv append norms and rotates q and k."""
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("rope_table", ctypes.c_void_p),
+                ("rope_len", ctypes.c_int), ("rot_dim", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("positions", ctypes.c_void_p),
+                ("num_axes", ctypes.c_int), ("sections", ctypes.c_int * 4)]
+
+
 class KvAttnError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"{_STATUS.get(code, code)}: {msg}")
@@ -83,6 +92,8 @@ def lib() -> ctypes.CDLL:
        i32, vp, sz, vp)
     _c(L.kvattn_prefill_chunk_fp8, i32, vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32,
        i32, i32, i32, f32, i32, vp, sz, vp)
+    _c(L.kvattn_qkv_append, i32, vp, sz, vp, sz, vp, sz, ctypes.POINTER(NormRope), vp, vp, vp, i32,
+       i32, i32, i32, i32, i32, i32, vp)
     _c(L.kvattn_step_map, i32, vp, vp, i32, vp, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp)
     _c(L.kvpool_granularity, i32, i32, ctypes.POINTER(ctypes.c_size_t))
     _c(L.kvpool_create, i32, i32, i32, sz, sz, ctypes.POINTER(vp))
@@ -413,6 +424,14 @@ def _require_fp8_layer(kv_layer, num_blocks: int, num_kv_heads: int, head_dim: i
             raise ValueError(f"kv_layer has {have} bytes, {num_blocks} blocks need {need}")
 
 
+def _require_layer(kv_layer, num_blocks: int, num_kv_heads: int, head_dim: int, esz: int):
+    if isinstance(kv_layer, torch.Tensor):
+        have = kv_layer.numel() * kv_layer.element_size()
+        need = int(num_blocks) * 2 * num_kv_heads * 16 * head_dim * esz
+        if have < need:
+            raise ValueError(f"kv_layer has {have} bytes, {num_blocks} blocks need {need}")
+
+
 def kv_append_fp8(k_new: torch.Tensor, v_new: torch.Tensor, slot_mapping: torch.Tensor, kv_layer,
                   num_blocks: int, *, block_size: int = 16, stream=None) -> None:
     """Write ``k_new``/``v_new`` [T, Hkv, d] (bf16 or fp32) into the slots ``slot_mapping``
@@ -484,6 +503,79 @@ def prefill_chunk_fp8(q: torch.Tensor, kv_layer, num_blocks: int, block_table: t
                                          float(scale), code, ws.data_ptr(), ws.numel(),
                                          _stream(stream)))
     return out
+
+
+def _qkv_append(call, q, k, v, slot_mapping, kv_layer, num_blocks, positions, rope_table,
+                sections, interleaved, q_weight, k_weight, eps, out, block_size, stream):
+    T, Hq, d = q.shape
+    Hkv = k.shape[1]
+    if k.shape != (T, Hkv, d) or v.shape != k.shape or not (q.dtype == k.dtype == v.dtype):
+        raise ValueError("q must be [T, Hq, d], k and v [T, Hkv, d], all of one dtype")
+    for x in (q, k, v):
+        if x.stride(2) != 1 or x.stride(1) != d and x.shape[1] > 1 or x.stride(0) < 0:
+            raise ValueError("a token's heads must be contiguous in q, k and v")
+    code = _dtype_code(q.dtype)
+    if slot_mapping.dtype != torch.int32 or slot_mapping.shape != (T,):
+        raise ValueError("slot_mapping must be int32 [num_tokens]")
+    prep = NormRope(eps=eps)
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            if w.dtype != q.dtype or w.shape != (d,):
+                raise ValueError(f"{name} must be [{d}] of q's dtype")
+            setattr(prep, name, w.data_ptr())
+    if rope_table is not None:
+        if rope_table.dtype != torch.float32 or rope_table.dim() != 2:
+            raise ValueError("rope_table must be float32 [positions, rot_dim]")
+        if positions is None or positions.dtype != torch.int32 or positions.shape[-1:] != (T,) or \
+                positions.dim() > 2:
+            raise ValueError("positions must be int32 [num_tokens] or [num_axes, num_tokens]")
+        prep.rope_table = rope_table.data_ptr()
+        prep.rope_len, prep.rot_dim = rope_table.shape
+        prep.interleaved = bool(interleaved)
+        prep.positions = positions.data_ptr()
+        prep.num_axes = axes = 1 if positions.dim() == 1 else positions.shape[0]
+        if sections is None:
+            if axes != 1:
+                raise ValueError("several axes of positions need sections")
+            sections = (rope_table.shape[1] // 2,)
+        if len(sections) != axes or axes > len(prep.sections):
+            raise ValueError(f"{axes} axes of positions, {len(sections)} sections (at most "
+                             f"{len(prep.sections)})")
+        prep.sections[:axes] = sections
+    elif positions is not None or sections is not None:
+        raise ValueError("positions and sections need a rope_table")
+    if out is not None and (out.dtype != q.dtype or out.shape != q.shape):
+        raise ValueError("out must have q's shape and dtype")
+    _require_here(slot_mapping, kv_layer, positions, rope_table, q_weight, k_weight, out)
+    here = slot_mapping.get_device()
+    if not (q.get_device() == k.get_device() == v.get_device() == here):
+        raise ValueError(f"q, k and v must be on slot_mapping's device (cuda:{here})")
+    if out is None:
+        out = _made_for(stream, lambda: torch.empty((T, Hq, d), dtype=q.dtype, device=q.device),
+                        returned=True)
+    check(call(q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
+               ctypes.byref(prep), slot_mapping.data_ptr(), out.data_ptr(), _ptr(kv_layer),
+               int(num_blocks), T, Hq, Hkv, d, int(block_size), code, _stream(stream)))
+    return out
+
+
+def qkv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slot_mapping: torch.Tensor,
+               kv_layer, num_blocks: int, *, positions: Optional[torch.Tensor] = None,
+               rope_table: Optional[torch.Tensor] = None, sections=None, interleaved: bool = False,
+               q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+               eps: float = 1e-6, out: Optional[torch.Tensor] = None, block_size: int = 16,
+               stream=None) -> torch.Tensor:
+    """Norm and rotate ``q`` [T, Hq, d] and ``k`` [T, Hkv, d], write ``k`` and ``v`` into the
+    slots ``slot_mapping`` [T] int32 of the layer, and return the new q [T, Hq, d].
+
+    ``q``, ``k`` and ``v`` may be views of one fused projection's output: a token's heads
+    must lie together, tokens may lie apart. ``q_weight`` and ``k_weight`` [d]: RMS norm of
+    each head. ``rope_table`` [positions, rot_dim] float32: cosines, then sines, looked up at
+    ``positions`` [T] int32 or, with ``sections`` (pairs of each axis), [axes, T]."""
+    _require_layer(kv_layer, num_blocks, k.shape[1], k.shape[2], k.element_size())
+    return _qkv_append(lib().kvattn_qkv_append, q, k, v, slot_mapping, kv_layer, num_blocks,
+                       positions, rope_table, sections, interleaved, q_weight, k_weight, eps, out,
+                       block_size, stream)
 
 
 class StepMap(NamedTuple):
