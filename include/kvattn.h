@@ -357,6 +357,15 @@ int kvattn_qkv_append(const void* q, size_t q_stride, const void* k, size_t k_st
                       int num_tokens, int num_q_heads, int num_kv_heads, int head_dim,
                       int block_size, kv_dtype dtype, void* stream);
 
+/* The same over a layer in 8 bits, same arguments, q, k and v in bf16 or fp32; K is scaled and
+ * rounded from the fp32 values that the rotation gives, V from its own, by the rules of
+ * kvattn_kv_append_fp8, which the order of slot_mapping follows too. */
+int kvattn_qkv_append_fp8(const void* q, size_t q_stride, const void* k, size_t k_stride,
+                          const void* v, size_t v_stride, const kvattn_norm_rope* prep,
+                          const int32_t* slot_mapping, void* q_out, void* kv_layer,
+                          int num_blocks, int num_tokens, int num_q_heads, int num_kv_heads,
+                          int head_dim, int block_size, kv_dtype dtype, void* stream);
+
 /* ------------------------------------------------------------------------- */
 /* The maps of a step on the GPU, from the requests' lengths: what append, decode and
  * prefill read, for layers of either format (Section 1: max_num_batched_tokens

@@ -678,6 +678,22 @@ extern "C" int kvattn_qkv_append(const void* q, size_t q_stride, const void* k, 
   return hip_status(kvattn::launch_qkv_append(a), fn);
 }
 
+extern "C" int kvattn_qkv_append_fp8(const void* q, size_t q_stride, const void* k, size_t k_stride,
+                                     const void* v, size_t v_stride, const kvattn_norm_rope* prep,
+                                     const int32_t* slot_mapping, void* q_out, void* kv_layer,
+                                     int num_blocks, int num_tokens, int num_q_heads,
+                                     int num_kv_heads, int head_dim, int block_size, kv_dtype dtype,
+                                     void* stream) {
+  clear_error();
+  const char* fn = "kvattn_qkv_append_fp8";
+  kvattn::QkvArgs a;
+  const int rc = qkv_check(fn, q, q_stride, k, k_stride, v, v_stride, prep, slot_mapping, q_out,
+                           kv_layer, num_blocks, num_tokens, num_q_heads, num_kv_heads, head_dim,
+                           block_size, dtype, true, stream, &a);
+  if (rc != KV_OK || num_tokens == 0) return rc;
+  return hip_status(kvattn::launch_qkv_append_fp8(a), fn);
+}
+
 extern "C" int kvattn_step_map(const int32_t* cached_lens, const int32_t* new_lens, int num_seqs,
                                const int32_t* free_ids, int num_free, int32_t* block_table,
                                int max_blocks_per_seq, int block_size, int max_tokens,

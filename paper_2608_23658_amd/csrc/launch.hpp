@@ -111,6 +111,7 @@ hipError_t launch_prefill(const PrefillArgs& a);
 hipError_t launch_append(const AppendArgs& a);
 hipError_t launch_append_fp8(const AppendArgs& a);
 hipError_t launch_qkv_append(const QkvArgs& a);
+hipError_t launch_qkv_append_fp8(const QkvArgs& a);
 hipError_t launch_step_map(const StepMapArgs& a);
 hipError_t launch_copy_blocks(const CopyArgs& a);
 

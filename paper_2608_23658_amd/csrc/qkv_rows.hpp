@@ -9,10 +9,17 @@
 // bf16 excepted: there they are two lanes of a row).
 #pragma once
 
+#include <type_traits>
+
 #include "common.hpp"
 #include "launch.hpp"
 
 namespace kvattn {
+
+namespace {
+constexpr int kRunTokens = 16;   // tokens of a run, slots of a block
+constexpr int kQkvWaves = 4;
+}  // namespace
 
 // kRot: registers of rotated chunks (0: no rotation). kEven: pairs are adjacent dims.
 template <int ESZ, int D, int kRot, bool kEven>
@@ -150,5 +157,123 @@ struct QkvRows {
     a = a1;
   }
 };
+
+// The work of workgroup wg, of (runs x groups of heads): per_wave heads a wavefront, of q
+// and, with kCache, k and v too.
+template <int ESZ, int D, int kRot, bool kEven, bool kCache>
+__device__ __forceinline__ void qkv_rows(const QkvArgs& a, int wg, int groups, int per_wave) {
+  using R = QkvRows<ESZ, D, kRot, kEven>;
+  const int lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int row = lane / 16;
+  const int hq = a.num_q_heads, hkv = a.num_kv_heads;
+  const int heads = kCache ? hq + 2 * hkv : hq;
+  const int h0 = (wg % groups * kQkvWaves + wave) * per_wave;
+  const int h1 = min(heads, h0 + per_wave);
+  if (h0 >= h1) return;
+  const int t = wg / groups * kRunTokens + lane % 16;
+  const bool real = t < a.num_tokens;
+  const int tc = min(t, a.num_tokens - 1);
+
+  R rows;
+  if (h0 < hq + hkv) rows.load_turns(a, tc);
+  uint8_t* block = nullptr;    // of the token's slot; null: it has none
+  int slot = 0;
+  constexpr size_t kTile = (size_t)kRunTokens * D * ESZ;
+  if (kCache && h1 > hq && real) {
+    slot = a.slot_mapping[t];
+    if ((unsigned)slot < (unsigned)(a.num_blocks * kRunTokens)) {
+      block = a.kv + (size_t)(slot / kRunTokens) * (2 * (size_t)hkv * kTile);
+      slot %= kRunTokens;
+    }
+  }
+
+  const uint8_t* weight = nullptr;
+  for (int h = h0; h < h1; ++h) {
+    const bool is_q = !kCache || h < hq, is_v = kCache && h >= hq + hkv;
+    const int g = is_q ? h : is_v ? h - hq - hkv : h - hq;
+    const uint8_t* src = (is_q ? a.q + (size_t)tc * a.q_stride
+                               : is_v ? a.v + (size_t)tc * a.v_stride
+                                      : a.k + (size_t)tc * a.k_stride) +
+                         (size_t)g * (D * ESZ);
+    uint4 raw[R::kN];
+#pragma unroll
+    for (int i = 0; i < R::kN; ++i) raw[i] = reinterpret_cast<const uint4*>(src)[4 * i + row];
+    if (!is_v) {
+      float x[R::kElems];
+#pragma unroll
+      for (int i = 0; i < R::kN; ++i) R::widen(raw[i], x + i * R::kVec);
+      const uint8_t* wanted = is_q ? a.q_weight : a.k_weight;
+      if (wanted) {
+        if (wanted != weight) rows.load_weight(wanted);
+        weight = wanted;
+        rows.norm(x, a.eps);
+      }
+      rows.rotate(x);
+#pragma unroll
+      for (int i = 0; i < R::kN; ++i) raw[i] = R::narrow(x + i * R::kVec);
+      if (is_q) {
+        if (real) {
+          uint4* to = reinterpret_cast<uint4*>(a.q_out + ((size_t)t * hq + g) * (D * ESZ));
+#pragma unroll
+          for (int i = 0; i < R::kN; ++i) to[4 * i + row] = raw[i];
+        }
+      } else if (block) {
+        uint4* to = reinterpret_cast<uint4*>(block + g * kTile);
+#pragma unroll
+        for (int i = 0; i < R::kN; ++i) to[(4 * i + row) * kRunTokens + slot] = raw[i];
+      }
+    } else if (block) {
+      uint8_t* to = block + (hkv + g) * kTile;
+#pragma unroll
+      for (int i = 0; i < R::kN; ++i) {
+        const uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+        const int j0 = (4 * i + row) * R::kVec;
+        if constexpr (ESZ == 2) {
+          uint16_t* v = reinterpret_cast<uint16_t*>(to);
+#pragma unroll
+          for (int e = 0; e < R::kVec; ++e)
+            v[(j0 + e) * kRunTokens + slot] = (uint16_t)(u[e / 2] >> (16 * (e % 2)));
+        } else {
+          uint32_t* v = reinterpret_cast<uint32_t*>(to);
+#pragma unroll
+          for (int e = 0; e < R::kVec; ++e) v[(j0 + e) * kRunTokens + slot] = u[e];
+        }
+      }
+    }
+  }
+}
+
+// How rows are dealt to wavefronts.
+struct QkvSplit {
+  int per_wave, groups;   // heads of a wavefront, workgroups of a run
+  long long workgroups;
+};
+inline QkvSplit qkv_split(int tokens, int heads) {
+  const long long runs = ((long long)tokens + kRunTokens - 1) / kRunTokens;
+  QkvSplit s;
+  s.per_wave = runs * heads > 16384 ? 4 : 1;
+  s.groups = (heads + kQkvWaves * s.per_wave - 1) / (kQkvWaves * s.per_wave);
+  s.workgroups = runs * s.groups;
+  return s;
+}
+
+// Calls launch with a call's rotated dims and whether its pairs are adjacent, as constants.
+template <int ESZ, int D, typename Launch>
+hipError_t with_rotation(const QkvArgs& a, Launch launch) {
+  const std::true_type even{};
+  const std::false_type halves{};
+  const std::integral_constant<int, 0> none{};
+  const std::integral_constant<int, 32> r32{};
+  const std::integral_constant<int, 64> r64{};
+  if (!a.table) return launch(none, halves);
+  if (a.rot == 32) return a.interleaved ? launch(r32, even) : launch(r32, halves);
+  if (a.rot == 64) return a.interleaved ? launch(r64, even) : launch(r64, halves);
+  if constexpr (D >= 128) {
+    const std::integral_constant<int, 128> r128{};
+    if (a.rot == 128) return a.interleaved ? launch(r128, even) : launch(r128, halves);
+  }
+  return hipErrorNotSupported;
+}
 
 }  // namespace kvattn

@@ -94,6 +94,8 @@ def lib() -> ctypes.CDLL:
        i32, i32, i32, f32, i32, vp, sz, vp)
     _c(L.kvattn_qkv_append, i32, vp, sz, vp, sz, vp, sz, ctypes.POINTER(NormRope), vp, vp, vp, i32,
        i32, i32, i32, i32, i32, i32, vp)
+    _c(L.kvattn_qkv_append_fp8, i32, vp, sz, vp, sz, vp, sz, ctypes.POINTER(NormRope), vp, vp, vp,
+       i32, i32, i32, i32, i32, i32, i32, vp)
     _c(L.kvattn_step_map, i32, vp, vp, i32, vp, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp)
     _c(L.kvpool_granularity, i32, i32, ctypes.POINTER(ctypes.c_size_t))
     _c(L.kvpool_create, i32, i32, i32, sz, sz, ctypes.POINTER(vp))
@@ -574,6 +576,21 @@ def qkv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slot_mapping: 
     ``positions`` [T] int32 or, with ``sections`` (pairs of each axis), [axes, T]."""
     _require_layer(kv_layer, num_blocks, k.shape[1], k.shape[2], k.element_size())
     return _qkv_append(lib().kvattn_qkv_append, q, k, v, slot_mapping, kv_layer, num_blocks,
+                       positions, rope_table, sections, interleaved, q_weight, k_weight, eps, out,
+                       block_size, stream)
+
+
+def qkv_append_fp8(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slot_mapping: torch.Tensor,
+                   kv_layer, num_blocks: int, *, positions: Optional[torch.Tensor] = None,
+                   rope_table: Optional[torch.Tensor] = None, sections=None,
+                   interleaved: bool = False, q_weight: Optional[torch.Tensor] = None,
+                   k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                   out: Optional[torch.Tensor] = None, block_size: int = 16,
+                   stream=None) -> torch.Tensor:
+    """``qkv_append`` into a layer in 8 bits; tokens of one block must stand together in
+    ``slot_mapping``."""
+    _require_fp8_layer(kv_layer, num_blocks, k.shape[1], k.shape[2])
+    return _qkv_append(lib().kvattn_qkv_append_fp8, q, k, v, slot_mapping, kv_layer, num_blocks,
                        positions, rope_table, sections, interleaved, q_weight, k_weight, eps, out,
                        block_size, stream)
 
