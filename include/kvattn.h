@@ -309,6 +309,43 @@ int kvattn_prefill_chunk_fp8(const void* q, const void* kv_layer, int num_blocks
                              void* stream);
 
 /* ------------------------------------------------------------------------- */
+/* Attention with other scores. The row at position p gives key t, for query head h,
+ *   a = scale * q . k
+ *   a = softcap * tanh(a / softcap)     if softcap > 0
+ *   a = a + slopes[h] * (t - p)         if slopes
+ * and sees the keys p - window < t <= p (window 0: 0 <= t <= p). */
+typedef struct {
+  float softcap;         /* 0: scores are not capped; else above zero, and scale / softcap as well
+                            as softcap finite after a factor of 3 */
+  const float* slopes;   /* device, [num_q_heads]; NULL: no bias */
+  int window;            /* keys a row sees, its own among them; 0: all up to its own */
+} kvattn_scoring;
+
+/* kvattn_decode and kvattn_decode_fp8 with such scores: same arguments, workspaces and
+ * rules, scoring (host, read before the call returns) beside scale, which may have any sign;
+ * scale * log2(e) must be finite. With a window, what is read of a sequence is the last
+ * window tokens: table entries of blocks wholly before them are not read, and what the
+ * window's first block holds before its first token has no effect, NaN included. A workspace
+ * for min(max_seq_len, window + 15) tokens is enough. The cap is within 2^-21 of it of
+ * softcap * tanh (near zero within 2^-21 of the value itself). A sequence's bits depend on
+ * itself, scoring and scale alone.
+ * Supported: as kvattn_decode (bf16 with head_dim 64 or 128, fp32 with 64) and
+ * kvattn_decode_fp8. */
+int kvattn_decode_scored(const void* q, const void* kv_layer, int num_blocks,
+                         const int32_t* block_table, const int32_t* seq_lens, void* out,
+                         int num_seqs, int num_q_heads, int num_kv_heads, int head_dim,
+                         int block_size, int max_blocks_per_seq, int max_seq_len, float scale,
+                         const kvattn_scoring* scoring, kv_dtype dtype, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+int kvattn_decode_scored_fp8(const void* q, const void* kv_layer, int num_blocks,
+                             const int32_t* block_table, const int32_t* seq_lens, void* out,
+                             int num_seqs, int num_q_heads, int num_kv_heads, int head_dim,
+                             int block_size, int max_blocks_per_seq, int max_seq_len, float scale,
+                             const kvattn_scoring* scoring, kv_dtype dtype, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------- */
 /* Between a layer's projection and its attention, in one launch: the norm of each q and
  * k head, their rotation by position, and the new K and V written into their paged slots
  * as kvattn_kv_append writes them.

@@ -15,6 +15,7 @@
 #include "kv_fp8.hpp"
 #include "kvattn.h"
 #include "launch.hpp"
+#include "scoring.hpp"
 
 namespace kvattn {
 
@@ -156,14 +157,14 @@ namespace {
 bool scale_log2_ok(float scale) { return std::isfinite(scale * kvattn::kLog2e); }
 
 // Checks a decode call and fills the launch descriptor; the workspace is
-// checked only when check_workspace is set.
+// checked only when check_workspace is set. most_tokens: of a context that are read.
 int decode_check(const char* fn, const void* q, const void* kv_layer, const void* kv2,
                  int num_base, int num_blocks, const int32_t* block_table,
                  const int32_t* seq_lens, void* out, int num_seqs, int num_q_heads,
                  int num_kv_heads, int head_dim, int block_size, int max_blocks_per_seq,
                  int max_seq_len, float scale, kv_dtype dtype, void* workspace,
                  size_t workspace_bytes, bool check_workspace, void* stream,
-                 kvattn::DecodeArgs* a, bool fp8 = false);
+                 kvattn::DecodeArgs* a, bool fp8 = false, int most_tokens = 0x7fffffff);
 
 int decode_launch(const char* fn, const kvattn::DecodeArgs& a);
 
@@ -251,7 +252,7 @@ int decode_check(const char* fn, const void* q, const void* kv_layer, const void
                  int num_kv_heads, int head_dim, int block_size, int max_blocks_per_seq,
                  int max_seq_len, float scale, kv_dtype dtype, void* workspace,
                  size_t workspace_bytes, bool check_workspace, void* stream,
-                 kvattn::DecodeArgs* out_args, bool fp8) {
+                 kvattn::DecodeArgs* out_args, bool fp8, int most_tokens) {
   if (num_seqs < 0) return set_error(KV_ERR_INVALID, "%s: num_seqs %d < 0", fn, num_seqs);
   if (dtype != KV_F32 && dtype != KV_BF16)
     return set_error(KV_ERR_INVALID, "%s: unknown dtype %d", fn, (int)dtype);
@@ -283,7 +284,7 @@ int decode_check(const char* fn, const void* q, const void* kv_layer, const void
   if (!aligned16(q) || !aligned16(kv_layer) || !aligned16(out))
     return set_error(KV_ERR_INVALID, "%s: q, kv_layer and out must be 16-byte aligned", fn);
   DecodeWs w;
-  decode_ws(num_seqs, num_q_heads, head_dim, max_seq_len, &w);
+  decode_ws(num_seqs, num_q_heads, head_dim, std::min(max_seq_len, most_tokens), &w);
   if (check_workspace) {
     if (!workspace) return set_error(KV_ERR_INVALID, "%s: null workspace", fn);
     if (!aligned16(workspace))
@@ -326,6 +327,76 @@ int decode_launch(const char* fn, const kvattn::DecodeArgs& a) {
 }
 
 }  // namespace
+
+namespace {
+// Checks what makes a call's scores; *mods: as the kernels take it.
+int scoring_check(const char* fn, const kvattn_scoring* s, float scale, kvattn::ScoreMods* mods) {
+  if (!s) return set_error(KV_ERR_INVALID, "%s: null scoring", fn);
+  if (!scale_log2_ok(scale))
+    return set_error(KV_ERR_INVALID, "%s: scale %g is not finite, or too large", fn, scale);
+  if (!(s->softcap >= 0.f) || !std::isfinite(2.f * kvattn::kLog2e * s->softcap))
+    return set_error(KV_ERR_INVALID, "%s: softcap %g", fn, s->softcap);
+  if (s->softcap > 0.f && !scale_log2_ok(2.f * (scale / s->softcap)))
+    return set_error(KV_ERR_INVALID, "%s: softcap %g is too small for scale %g", fn, s->softcap,
+                     scale);
+  if (s->window < 0) return set_error(KV_ERR_INVALID, "%s: window %d", fn, s->window);
+  if (reinterpret_cast<uintptr_t>(s->slopes) & 3)
+    return set_error(KV_ERR_INVALID, "%s: slopes must be 4-byte aligned", fn);
+  *mods = {s->softcap, s->slopes, s->window};
+  return KV_OK;
+}
+
+int decode_scored_common(const char* fn, bool fp8, const void* q, const void* kv_layer,
+                         int num_blocks, const int32_t* block_table, const int32_t* seq_lens,
+                         void* out, int num_seqs, int num_q_heads, int num_kv_heads, int head_dim,
+                         int block_size, int max_blocks_per_seq, int max_seq_len, float scale,
+                         const kvattn_scoring* scoring, kv_dtype dtype, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  kvattn::ScoreMods mods;
+  int rc = scoring_check(fn, scoring, scale, &mods);
+  if (rc != KV_OK) return rc;
+  const int most = mods.window > 0 ? std::min(mods.window, kvattn::kNoWindow) + 15 : 0x7fffffff;
+  kvattn::DecodeArgs a;
+  rc = decode_check(fn, q, kv_layer, nullptr, 0, num_blocks, block_table, seq_lens, out, num_seqs,
+                    num_q_heads, num_kv_heads, head_dim, block_size, max_blocks_per_seq,
+                    max_seq_len, scale, dtype, workspace, workspace_bytes, true, stream, &a, fp8,
+                    most);
+  if (rc != KV_OK || num_seqs == 0) return rc;
+  a.mods = &mods;
+  return hip_status(kvattn::launch_decode_scored(a), fn);
+}
+}  // namespace
+
+extern "C" int kvattn_decode_scored(const void* q, const void* kv_layer, int num_blocks,
+                                    const int32_t* block_table, const int32_t* seq_lens,
+                                    void* out, int num_seqs, int num_q_heads, int num_kv_heads,
+                                    int head_dim, int block_size, int max_blocks_per_seq,
+                                    int max_seq_len, float scale, const kvattn_scoring* scoring,
+                                    kv_dtype dtype, void* workspace, size_t workspace_bytes,
+                                    void* stream) {
+  clear_error();
+  return decode_scored_common("kvattn_decode_scored", false, q, kv_layer, num_blocks, block_table,
+                              seq_lens, out, num_seqs, num_q_heads, num_kv_heads, head_dim,
+                              block_size, max_blocks_per_seq, max_seq_len, scale, scoring, dtype,
+                              workspace, workspace_bytes, stream);
+}
+
+extern "C" int kvattn_decode_scored_fp8(const void* q, const void* kv_layer, int num_blocks,
+                                        const int32_t* block_table, const int32_t* seq_lens,
+                                        void* out, int num_seqs, int num_q_heads,
+                                        int num_kv_heads, int head_dim, int block_size,
+                                        int max_blocks_per_seq, int max_seq_len, float scale,
+                                        const kvattn_scoring* scoring, kv_dtype dtype,
+                                        void* workspace, size_t workspace_bytes, void* stream) {
+  clear_error();
+  const char* fn = "kvattn_decode_scored_fp8";
+  if (dtype == KV_F32)
+    return set_error(KV_ERR_UNSUPPORTED, "%s: fp32 queries are not built", fn);
+  return decode_scored_common(fn, true, q, kv_layer, num_blocks, block_table, seq_lens, out,
+                              num_seqs, num_q_heads, num_kv_heads, head_dim, block_size,
+                              max_blocks_per_seq, max_seq_len, scale, scoring, dtype, workspace,
+                              workspace_bytes, stream);
+}
 
 namespace {
 // The least a prefill call takes: the list of whole work tiles, one int2 per

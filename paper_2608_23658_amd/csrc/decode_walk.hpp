@@ -4,6 +4,7 @@
 #pragma once
 
 #include "common.hpp"
+#include "scoring.hpp"
 
 namespace kvattn {
 
@@ -121,13 +122,16 @@ __device__ __forceinline__ void load_step(const DecodeTiles<kTwo>& t, const int 
 //     of the two blocks' V loads gives the matching A operands of 16 dims each.
 // kAhead: the next step's loads are issued before a step's products, into a
 // second set of registers; at most 64 blocks, whose ids one load gives.
+// score: how a score is made; with ModScore the query is token `own`, its heads are h0 on
+// and it sees tokens from lo on (a walk begins at most 15 before it; what they hold may
+// be anything).
 // Leaves the wavefront's state in o_out [G][D] and ml_out [G] (LDS).
-template <int D, int G, bool kTwo, bool kAhead>
+template <int D, int G, bool kTwo, bool kAhead, class Score>
 __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
                                           const uint16_t* __restrict__ q,
                                           const int* __restrict__ bt, int num_blocks, int t0,
-                                          int t1, float scale_log2, float* o_out,
-                                          float2* ml_out) {
+                                          int t1, const Score& score, float* o_out, float2* ml_out,
+                                          int h0 = 0, int own = 0, int lo = 0) {
   using S = DecodeShape<D, true>;
   const int lane = threadIdx.x % kWave;
   const int head = lane % 16, row = lane / 16;
@@ -139,6 +143,8 @@ __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
     if (head >= G) qreg[i] = make_uint4(0, 0, 0, 0);
   }
 
+  float slope = 0.f;
+  if constexpr (Score::kOn) slope = score.slope(h0 + min(head, G - 1));
   float m_run = -INFINITY, l_run = 0.f;   // head's max; the lane's part of its sum
   f32x4_t acc[2 * S::kVI];
 #pragma unroll
@@ -163,8 +169,13 @@ __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
                                                      0, 0);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const bool keep = bid[j] >= 0 && (!tail || tb + j * S::kBS + row * 4 + r < t1);
-        x[j][r] = keep ? sc[r] * scale_log2 : -INFINITY;
+        const int tok = tb + j * S::kBS + row * 4 + r;
+        const bool keep = bid[j] >= 0 && (!tail || tok < t1);
+        if constexpr (Score::kOn)
+          x[j][r] = keep && tok >= lo ? score.template at<false>(sc[r], slope, own - tok)
+                                      : -INFINITY;
+        else
+          x[j][r] = keep ? sc[r] * score.scale_log2 : -INFINITY;
       }
     }
 
@@ -201,19 +212,20 @@ __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
         for (int i = 0; i < S::kVI; ++i) vreg[j][i] = make_uint4(0, 0, 0, 0);
       }
     }
-    if (tail) {
+    if (tail || (Score::kOn && tb < lo)) {
 #pragma unroll
       for (int j = 0; j < S::kTB; ++j) {
-        // slots at or past t1 may hold anything, and zero times NaN is NaN
+        // slots at or past t1 (or before lo) may hold anything, and zero times NaN is NaN
         const int tok = tb + j * S::kBS + (lane / 32) * 8;
+        auto seen = [&](int t) { return t < t1 && (!Score::kOn || t >= lo); };
 #pragma unroll
         for (int i = 0; i < S::kVI; ++i) {
           uint32_t w[4] = {vreg[j][i].x, vreg[j][i].y, vreg[j][i].z, vreg[j][i].w};
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const uint32_t lo = (tok + 2 * k < t1) ? 0x0000ffffu : 0u;
-            const uint32_t hi = (tok + 2 * k + 1 < t1) ? 0xffff0000u : 0u;
-            w[k] &= (lo | hi);
+            const uint32_t lo16 = seen(tok + 2 * k) ? 0x0000ffffu : 0u;
+            const uint32_t hi16 = seen(tok + 2 * k + 1) ? 0xffff0000u : 0u;
+            w[k] &= (lo16 | hi16);
           }
           vreg[j][i] = make_uint4(w[0], w[1], w[2], w[3]);
         }

@@ -75,10 +75,11 @@ struct Fp8Tiles {
 // the tokens are those whose scores the lane has, so nothing is exchanged
 // between lanes. The conversions (32 a block) take the place of the lane swaps
 // that the bf16 walk needs there.
-template <int D, int G, bool kAhead>
+template <int D, int G, bool kAhead, class Score>
 __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* __restrict__ q,
                                          const int* __restrict__ bt, int num_blocks, int t0,
-                                         int t1, float scale_log2, float* o_out, float2* ml_out) {
+                                         int t1, const Score& score, float* o_out, float2* ml_out,
+                                         int h0 = 0, int own = 0, int lo = 0) {
   constexpr int kBS = 16, kTile = 64, kTB = kTile / kBS;
   constexpr int kL = D / 64;   // loads per tile
   const int lane = threadIdx.x % kWave;
@@ -99,6 +100,8 @@ __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* 
       qreg[i][b] = __builtin_bit_cast(bf16x8_t, v);
     }
 
+  float slope = 0.f;
+  if constexpr (Score::kOn) slope = score.slope(h0 + min(head, G - 1));
   float m_run = -INFINITY, l_run = 0.f;   // head's max; the lane's part of its sum
   f32x4_t acc[4 * kL];
 #pragma unroll
@@ -149,8 +152,13 @@ __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* 
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const bool keep = bid[j] >= 0 && (!tail || tb + j * kBS + row * 4 + r < t1);
-        x[j][r] = keep ? sc[r] * scale_log2 : -INFINITY;
+        const int tok = tb + j * kBS + row * 4 + r;
+        const bool keep = bid[j] >= 0 && (!tail || tok < t1);
+        if constexpr (Score::kOn)
+          x[j][r] = keep && tok >= lo ? score.template at<false>(sc[r], slope, own - tok)
+                                      : -INFINITY;
+        else
+          x[j][r] = keep ? sc[r] * score.scale_log2 : -INFINITY;
       }
     }
 
@@ -189,11 +197,13 @@ __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* 
         for (int i = 0; i < kL; ++i) vreg[j][i] = make_uint4(0, 0, 0, 0);
       }
     }
-    if (tail) {
-      // slots at or past t1 may hold anything, and zero times NaN is NaN
+    if (tail || (Score::kOn && tb < lo)) {
+      // slots at or past t1 (or before lo) may hold anything, and zero times NaN is NaN
 #pragma unroll
       for (int j = 0; j < kTB; ++j) {
-        const uint32_t keep = first_bytes(t1 - (tb + j * kBS + row * 4));
+        const int tok = tb + j * kBS + row * 4;
+        uint32_t keep = first_bytes(t1 - tok);
+        if constexpr (Score::kOn) keep &= ~first_bytes(lo - tok);
 #pragma unroll
         for (int i = 0; i < kL; ++i) {
           const uint4 v = vreg[j][i];

@@ -10,6 +10,13 @@ namespace kvattn {
 constexpr int kDecodeWaves = 4;     // wavefronts that share one split of a context
 constexpr int kSpreadBlocks = 128;  // most splits x kv heads given a workgroup per wavefront
 
+// What makes a call's scores other than scale * q . k.
+struct ScoreMods {
+  float softcap;         // 0: none
+  const float* slopes;   // of every query head; null: no bias
+  int window;            // 0: none
+};
+
 struct DecodeArgs {
   const void* q;
   const void* kv;
@@ -24,6 +31,7 @@ struct DecodeArgs {
   float scale;
   bool bf16;         // q, out and the cache; with fp8 q and out
   bool fp8 = false;  // the cache is in 8 bits
+  const ScoreMods* mods = nullptr;   // null: plain scores
   void* workspace;
   size_t ws_ml_offset;   // byte offset of the (m, l) partials in the workspace
   // The same with a partial per wavefront of a split; 0: the workspace has no
@@ -44,6 +52,7 @@ struct PrefillArgs {
   int max_blocks, max_seq_len;
   float scale;
   bool fp8 = false;   // the cache is in 8 bits
+  const ScoreMods* mods = nullptr;   // null: plain scores
   void* workspace;
   size_t workspace_bytes;
   hipStream_t stream;
@@ -107,6 +116,7 @@ void trace_before(hipStream_t stream, const char* kernel);
 void trace_after(hipStream_t stream);
 
 hipError_t launch_decode(const DecodeArgs& a);
+hipError_t launch_decode_scored(const DecodeArgs& a);   // with a.mods
 hipError_t launch_prefill(const PrefillArgs& a);
 hipError_t launch_append(const AppendArgs& a);
 hipError_t launch_append_fp8(const AppendArgs& a);

@@ -48,6 +48,12 @@ class NormRope(ctypes.Structure):
                 ("num_axes", ctypes.c_int), ("sections", ctypes.c_int * 4)]
 
 
+class Scoring(ctypes.Structure):
+    """``kvattn_scoring``: how the scored attention calls make a score of q . k."""
+    _fields_ = [("softcap", ctypes.c_float), ("slopes", ctypes.c_void_p),
+                ("window", ctypes.c_int)]
+
+
 class KvAttnError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"{_STATUS.get(code, code)}: {msg}")
@@ -92,6 +98,10 @@ def lib() -> ctypes.CDLL:
        i32, vp, sz, vp)
     _c(L.kvattn_prefill_chunk_fp8, i32, vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32,
        i32, i32, i32, f32, i32, vp, sz, vp)
+    sc = ctypes.POINTER(Scoring)
+    for f in (L.kvattn_decode_scored, L.kvattn_decode_scored_fp8):
+        _c(f, i32, vp, vp, i32, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, f32, sc, i32, vp, sz,
+           vp)
     _c(L.kvattn_qkv_append, i32, vp, sz, vp, sz, vp, sz, ctypes.POINTER(NormRope), vp, vp, vp, i32,
        i32, i32, i32, i32, i32, i32, vp)
     _c(L.kvattn_qkv_append_fp8, i32, vp, sz, vp, sz, vp, sz, ctypes.POINTER(NormRope), vp, vp, vp,
@@ -505,6 +515,62 @@ def prefill_chunk_fp8(q: torch.Tensor, kv_layer, num_blocks: int, block_table: t
                                          float(scale), code, ws.data_ptr(), ws.numel(),
                                          _stream(stream)))
     return out
+
+
+def _scoring(softcap, slopes, window: int, num_q_heads: int):
+    if slopes is None:
+        return Scoring(softcap, None, window)
+    if slopes.dtype != torch.float32 or slopes.shape != (num_q_heads,):
+        raise ValueError(f"slopes must be float32 [{num_q_heads}]")
+    return Scoring(softcap, slopes.data_ptr(), window)
+
+
+def _decode_scored(call, q, kv_layer, num_blocks, block_table, seq_lens, num_kv_heads, max_seq_len,
+                   softcap, slopes, window, block_size, scale, out, ws, stream):
+    B, Hq, d = q.shape
+    _require_batch(B, block_table, seq_lens)
+    _require_out(out, q)
+    code = _dtype_code(q.dtype)
+    scoring = _scoring(softcap, slopes, window, Hq)
+    _require_here(q, kv_layer, block_table, seq_lens, slopes, out, ws)
+    if out is None:
+        out = _made_for(stream, torch.empty_like, q, returned=True)
+    if ws is None:
+        most = min(max_seq_len, window + 15) if window > 0 else max_seq_len
+        ws = _made_for(stream, workspace, decode_workspace_bytes(B, Hq, d, most), q.device)
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    check(call(q.data_ptr(), _ptr(kv_layer), int(num_blocks), block_table.data_ptr(),
+               seq_lens.data_ptr(), out.data_ptr(), B, Hq, int(num_kv_heads), d, int(block_size),
+               int(block_table.shape[1]), int(max_seq_len), float(scale), scoring, code,
+               ws.data_ptr(), ws.numel(), _stream(stream)))
+    return out
+
+
+def decode_scored(q: torch.Tensor, kv_layer, num_blocks: int, block_table: torch.Tensor,
+                  seq_lens: torch.Tensor, *, num_kv_heads: int, max_seq_len: int,
+                  softcap: float = 0.0, slopes: Optional[torch.Tensor] = None, window: int = 0,
+                  block_size: int = 16, scale: Optional[float] = None,
+                  out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """``decode`` with other scores: capped at ``softcap`` by a tanh (0: not), biased by
+    ``slopes`` [Hq] float32 times the distance, over the last ``window`` tokens (0: all)."""
+    _require_layer(kv_layer, num_blocks, num_kv_heads, q.shape[2], q.element_size())
+    return _decode_scored(lib().kvattn_decode_scored, q, kv_layer, num_blocks, block_table,
+                          seq_lens, num_kv_heads, max_seq_len, softcap, slopes, window, block_size,
+                          scale, out, ws, stream)
+
+
+def decode_scored_fp8(q: torch.Tensor, kv_layer, num_blocks: int, block_table: torch.Tensor,
+                      seq_lens: torch.Tensor, *, num_kv_heads: int, max_seq_len: int,
+                      softcap: float = 0.0, slopes: Optional[torch.Tensor] = None, window: int = 0,
+                      block_size: int = 16, scale: Optional[float] = None,
+                      out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                      stream=None) -> torch.Tensor:
+    """``decode_scored`` over a layer in 8 bits: ``q`` [B, Hq, d] bf16."""
+    _require_fp8_layer(kv_layer, num_blocks, num_kv_heads, q.shape[2])
+    return _decode_scored(lib().kvattn_decode_scored_fp8, q, kv_layer, num_blocks, block_table,
+                          seq_lens, num_kv_heads, max_seq_len, softcap, slopes, window, block_size,
+                          scale, out, ws, stream)
 
 
 def _qkv_append(call, q, k, v, slot_mapping, kv_layer, num_blocks, positions, rope_table,
