@@ -345,6 +345,32 @@ int kvattn_decode_scored_fp8(const void* q, const void* kv_layer, int num_blocks
                              const kvattn_scoring* scoring, kv_dtype dtype, void* workspace,
                              size_t workspace_bytes, void* stream);
 
+/* kvattn_prefill_chunk and kvattn_prefill_chunk_fp8 with such scores: same arguments,
+ * workspaces and rules but that scale may have any sign (scale * log2(e) finite). With a
+ * window, table entries of blocks wholly before the window of a chunk's first row are not
+ * used for anything, and what lies before it in that window's first block has no effect,
+ * NaN included. A row that sees no key (its ids outside the layer) gets zeros. Rows behind
+ * cu_seqlens_q[num_seqs] are left as they are. What a row's bits depend on is as said there,
+ * but that what a window leaves out of a tile or sequence does not count for its length.
+ * Supported: as those (head_dim 128). */
+int kvattn_prefill_chunk_scored(const void* q, const void* kv_layer, int num_blocks,
+                                const int32_t* block_table, const int32_t* seq_lens,
+                                const int32_t* cu_seqlens_q, void* out, int num_seqs,
+                                int total_q_tokens, int max_num_batched_tokens,
+                                int num_q_heads, int num_kv_heads, int head_dim,
+                                int block_size, int max_blocks_per_seq, int max_seq_len,
+                                float scale, const kvattn_scoring* scoring, kv_dtype dtype,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+int kvattn_prefill_chunk_scored_fp8(const void* q, const void* kv_layer, int num_blocks,
+                                    const int32_t* block_table, const int32_t* seq_lens,
+                                    const int32_t* cu_seqlens_q, void* out, int num_seqs,
+                                    int total_q_tokens, int max_num_batched_tokens,
+                                    int num_q_heads, int num_kv_heads, int head_dim,
+                                    int block_size, int max_blocks_per_seq, int max_seq_len,
+                                    float scale, const kvattn_scoring* scoring, kv_dtype dtype,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------------- */
 /* Between a layer's projection and its attention, in one launch: the norm of each q and
  * k head, their rotation by position, and the new K and V written into their paged slots

@@ -24,7 +24,8 @@ ARCH = "gfx950"
 SOURCES = ["abi.cpp", "kvpool.cpp", "blockpool.cpp", "decode.hip", "prefill.hip", "append.hip",
            "blocks.hip", "probes.hip",
            "append_fp8.hip", "prefill_fp8.hip", "step_map.hip", "qkv_append.hip",
-           "qkv_append_fp8.hip", "decode_scored.hip"]
+           "qkv_append_fp8.hip", "decode_scored.hip",
+           "prefill_scored.hip", "prefill_capped.hip", "prefill_scored_fp8.hip"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", "-Werror=inline-asm",
           "-I", INCLUDE, "-I", CSRC]

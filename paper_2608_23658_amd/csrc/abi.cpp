@@ -419,7 +419,8 @@ int prefill_common(const char* fn, bool fp8, const void* q, const void* kv_layer
                    const int32_t* cu_seqlens_q, void* out, int num_seqs, int total_q_tokens,
                    int max_num_batched_tokens, int num_q_heads, int num_kv_heads, int head_dim,
                    int block_size, int max_blocks_per_seq, int max_seq_len, float scale,
-                   kv_dtype dtype, void* workspace, size_t workspace_bytes, void* stream) {
+                   kv_dtype dtype, void* workspace, size_t workspace_bytes, void* stream,
+                   const kvattn::ScoreMods* mods = nullptr) {
   if (dtype == KV_F32)
     return set_error(KV_ERR_UNSUPPORTED, "%s: fp32 prefill is not built", fn);
   if (dtype != KV_BF16)
@@ -453,8 +454,8 @@ int prefill_common(const char* fn, bool fp8, const void* q, const void* kv_layer
     return set_error(KV_ERR_INVALID, "%s: scale not finite", fn);
   if (fp8 && !scale_log2_ok(scale))
     return set_error(KV_ERR_INVALID, "%s: scale %g is too large", fn, scale);
-  // masked scores are minus infinity before the scale
-  if (fp8 && !(scale > 0.f))
+  // masked scores are minus infinity before the scale (with mods, after one below zero)
+  if (fp8 && !mods && !(scale > 0.f))
     return set_error(KV_ERR_INVALID, "%s: scale %g must be above zero", fn, scale);
   if (num_kv_heads > 65535) return set_error(KV_ERR_UNSUPPORTED, "%s: grid", fn);
   if (num_seqs == 0 || total_q_tokens == 0) return KV_OK;
@@ -484,6 +485,7 @@ int prefill_common(const char* fn, bool fp8, const void* q, const void* kv_layer
   a.max_seq_len = max_seq_len;
   a.scale = scale;
   a.fp8 = fp8;
+  a.mods = mods;
   a.workspace = workspace;
   a.workspace_bytes = workspace_bytes;
   a.stream = static_cast<hipStream_t>(stream);
@@ -522,6 +524,46 @@ extern "C" int kvattn_prefill_chunk_fp8(const void* q, const void* kv_layer, int
                         seq_lens, cu_seqlens_q, out, num_seqs, total_q_tokens, max_num_batched_tokens,
                         num_q_heads, num_kv_heads, head_dim, block_size, max_blocks_per_seq,
                         max_seq_len, scale, dtype, workspace, workspace_bytes, stream);
+}
+
+extern "C" int kvattn_prefill_chunk_scored(const void* q, const void* kv_layer, int num_blocks,
+                                           const int32_t* block_table, const int32_t* seq_lens,
+                                           const int32_t* cu_seqlens_q, void* out, int num_seqs,
+                                           int total_q_tokens, int max_num_batched_tokens,
+                                           int num_q_heads, int num_kv_heads, int head_dim,
+                                           int block_size, int max_blocks_per_seq,
+                                           int max_seq_len, float scale,
+                                           const kvattn_scoring* scoring, kv_dtype dtype,
+                                           void* workspace, size_t workspace_bytes, void* stream) {
+  clear_error();
+  const char* fn = "kvattn_prefill_chunk_scored";
+  kvattn::ScoreMods mods;
+  const int rc = scoring_check(fn, scoring, scale, &mods);
+  if (rc != KV_OK) return rc;
+  return prefill_common(fn, false, q, kv_layer, num_blocks, block_table, seq_lens, cu_seqlens_q,
+                        out, num_seqs, total_q_tokens, max_num_batched_tokens, num_q_heads,
+                        num_kv_heads, head_dim, block_size, max_blocks_per_seq, max_seq_len, scale,
+                        dtype, workspace, workspace_bytes, stream, &mods);
+}
+
+extern "C" int kvattn_prefill_chunk_scored_fp8(const void* q, const void* kv_layer, int num_blocks,
+                                               const int32_t* block_table, const int32_t* seq_lens,
+                                               const int32_t* cu_seqlens_q, void* out, int num_seqs,
+                                               int total_q_tokens, int max_num_batched_tokens,
+                                               int num_q_heads, int num_kv_heads, int head_dim,
+                                               int block_size, int max_blocks_per_seq,
+                                               int max_seq_len, float scale,
+                                               const kvattn_scoring* scoring, kv_dtype dtype,
+                                               void* workspace, size_t workspace_bytes, void* stream) {
+  clear_error();
+  const char* fn = "kvattn_prefill_chunk_scored_fp8";
+  kvattn::ScoreMods mods;
+  const int rc = scoring_check(fn, scoring, scale, &mods);
+  if (rc != KV_OK) return rc;
+  return prefill_common(fn, true, q, kv_layer, num_blocks, block_table, seq_lens, cu_seqlens_q,
+                        out, num_seqs, total_q_tokens, max_num_batched_tokens, num_q_heads,
+                        num_kv_heads, head_dim, block_size, max_blocks_per_seq, max_seq_len, scale,
+                        dtype, workspace, workspace_bytes, stream, &mods);
 }
 
 extern "C" int kvattn_kv_append(const void* k_new, const void* v_new,

@@ -16,7 +16,7 @@ hipError_t launch_decode(const DecodeArgs& a) {
       default: return hipErrorInvalidValue;
     }
   }
-  return dispatch_decode(a, score);
+  return a.bf16 ? dispatch_bf16(a, score) : dispatch_f32(a, score);
 }
 
 }  // namespace kvattn

@@ -5,7 +5,10 @@
 namespace kvattn {
 
 hipError_t launch_decode_scored(const DecodeArgs& a) {
-  return dispatch_decode(a, mod_score(a.scale, *a.mods));
+  if (a.bf16) return dispatch_bf16(a, mod_score<Cap::kAsk>(a.scale, *a.mods));
+  // with the library's tanh, fp32's walk is built with a cap and without
+  return a.mods->softcap > 0.f ? dispatch_f32(a, mod_score<Cap::kYes>(a.scale, *a.mods))
+                               : dispatch_f32(a, mod_score<Cap::kNo>(a.scale, *a.mods));
 }
 
 }  // namespace kvattn

@@ -151,8 +151,9 @@ __device__ __forceinline__ void wave_lds_sync() {
 template <int D, int G, class Score>
 __device__ __forceinline__ void walk_f32(const DecodeTiles<false>& tiles, const uint4* q_lds,
                                          float* p_lds, int my_id, int t0, int t1,
-                                         const Score& score, float* o_out, float2* ml_out,
+                                         const Score& how, float* o_out, float2* ml_out,
                                          float* whole_out, int h0 = 0, int own = 0, int lo = 0) {
+  const auto& score = how.held();
   using S = DecodeShape<D, false>;
   const int lane = threadIdx.x % kWave;
   float m_run[G], l_run[G], acc[S::kVI][G];
@@ -166,7 +167,10 @@ __device__ __forceinline__ void walk_f32(const DecodeTiles<false>& tiles, const 
   float slope[G];
   if constexpr (Score::kOn) {
 #pragma unroll
-    for (int h = 0; h < G; ++h) slope[h] = score.slope(h0 + h);
+    for (int h = 0; h < G; ++h) {
+      slope[h] = score.slope(h0 + h);
+      asm("" : "+v"(slope[h]));   // as held()
+    }
   }
   // block of this lane's token within the step, and which quarter of the K
   // rows of its slot the lane holds
@@ -661,7 +665,8 @@ __global__ __launch_bounds__(kCombineWaves * kWave) void decode_combine_kernel(
 
 // The most tokens a call walks of a sequence: a window's, and those before it in its block.
 inline int most_tokens(const DecodeArgs& a, const PlainScore&) { return a.max_seq_len; }
-inline int most_tokens(const DecodeArgs& a, const ModScore& s) {
+template <Cap kCap>
+int most_tokens(const DecodeArgs& a, const ModScore<kCap>& s) {
   return std::min(a.max_seq_len, s.window + 15);
 }
 
@@ -682,7 +687,9 @@ static hipError_t launch_decode_t(const DecodeArgs& a, const Score& score) {
   // so further wavefronts would only wait.
   const int steps = (most + kStepTokens - 1) / kStepTokens;
   int waves = spread || steps < 1 ? 1 : steps < kDecodeWaves ? steps : kDecodeWaves;
-  const bool turns = waves == kDecodeWaves &&
+  // (fp32's walk with other scores has no scalar registers left for the turns)
+  constexpr bool kCanTurn = BF16 || !Score::kOn;
+  const bool turns = kCanTurn && waves == kDecodeWaves &&
                      (blocks > kFullBlocks ||
                       (!BF16 && steps <= kShortSteps && blocks >= kShortBlocks));
   if (turns) {
@@ -692,7 +699,8 @@ static hipError_t launch_decode_t(const DecodeArgs& a, const Score& score) {
     blocks = per_piece * std::min<long long>(splits, pieces);
   }
   auto split = decode_split_kernel<D, G, BF16, kTwo, false, false, false, kFp8, Score>;
-  if (turns) split = decode_split_kernel<D, G, BF16, kTwo, false, false, true, kFp8, Score>;
+  if constexpr (kCanTurn)
+    if (turns) split = decode_split_kernel<D, G, BF16, kTwo, false, false, true, kFp8, Score>;
   if constexpr (kCanSpread) {
     if (spread)
       split = decode_split_kernel<D, G, BF16, kTwo, true, true, false, kFp8, Score>;
@@ -746,15 +754,19 @@ static hipError_t dispatch_g(const DecodeArgs& a, const Score& score) {
 }
 
 template <class Score>
-static hipError_t dispatch_decode(const DecodeArgs& a, const Score& score) {
+static hipError_t dispatch_f32(const DecodeArgs& a, const Score& score) {
+  return a.head_dim == 64 ? dispatch_g<64, false, false>(a, score) : hipErrorInvalidValue;
+}
+
+// Over a bf16 cache or one in 8 bits.
+template <class Score>
+static hipError_t dispatch_bf16(const DecodeArgs& a, const Score& score) {
   if (a.fp8) {
     if (a.head_dim == 128) return dispatch_g<128, true, true>(a, score);
     if (a.head_dim == 64) return dispatch_g<64, true, true>(a, score);
-  } else if (a.bf16) {
+  } else {
     if (a.head_dim == 128) return dispatch_g<128, true, false>(a, score);
     if (a.head_dim == 64) return dispatch_g<64, true, false>(a, score);
-  } else {
-    if (a.head_dim == 64) return dispatch_g<64, false, false>(a, score);
   }
   return hipErrorInvalidValue;
 }

@@ -130,8 +130,9 @@ template <int D, int G, bool kTwo, bool kAhead, class Score>
 __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
                                           const uint16_t* __restrict__ q,
                                           const int* __restrict__ bt, int num_blocks, int t0,
-                                          int t1, const Score& score, float* o_out, float2* ml_out,
+                                          int t1, const Score& how, float* o_out, float2* ml_out,
                                           int h0 = 0, int own = 0, int lo = 0) {
+  const auto& score = how.held();
   using S = DecodeShape<D, true>;
   const int lane = threadIdx.x % kWave;
   const int head = lane % 16, row = lane / 16;

@@ -78,8 +78,9 @@ struct Fp8Tiles {
 template <int D, int G, bool kAhead, class Score>
 __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* __restrict__ q,
                                          const int* __restrict__ bt, int num_blocks, int t0,
-                                         int t1, const Score& score, float* o_out, float2* ml_out,
+                                         int t1, const Score& how, float* o_out, float2* ml_out,
                                          int h0 = 0, int own = 0, int lo = 0) {
+  const auto& score = how.held();
   constexpr int kBS = 16, kTile = 64, kTB = kTile / kBS;
   constexpr int kL = D / 64;   // loads per tile
   const int lane = threadIdx.x % kWave;

@@ -129,8 +129,8 @@ hipError_t launch_copy_blocks(const CopyArgs& a);
 // size 8; the workspace's tile list is sized for it.
 constexpr int kPrefillRows = 32;
 
-// The attention kernel of a chunked-prefill call over a cache in 8 bits, for the
-// items of a plan (head) or the whole tiles of a tile map.
+// The attention kernel of a chunked-prefill call over a cache in 8 bits, or with other
+// scores (a.mods), for the items of a plan (head) or the whole tiles of a tile map.
 struct PrefillItem;
 struct PrefillPlan;
 struct PrefillLaunch {
@@ -142,6 +142,9 @@ struct PrefillLaunch {
   uint8_t *slots, *row_slots;
 };
 hipError_t launch_prefill_fp8(const PrefillArgs& a, const PrefillLaunch& l);
+hipError_t launch_prefill_scored(const PrefillArgs& a, const PrefillLaunch& l);
+hipError_t launch_prefill_capped(const PrefillArgs& a, const PrefillLaunch& l);   // of those
+hipError_t launch_prefill_scored_fp8(const PrefillArgs& a, const PrefillLaunch& l);
 
 // Workspace of a planned prefill step, whatever its kv head count.
 size_t prefill_planned_bytes(int num_seqs, int total_q_tokens, int num_q_heads);

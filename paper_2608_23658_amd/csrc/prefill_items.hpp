@@ -114,6 +114,32 @@ struct PrefillItem {
   int cu0, n, L;    // the sequence's chunk and clamped length
 };
 
+// First key step, an even one, of a tile whose first row is at position pos, where a
+// row sees window keys.
+__device__ __forceinline__ int first_step(int pos, int window) {
+  return max(0, pos - window + 1) / kKeys & ~1;
+}
+
+// The item of workgroup (ti, kv head) of a launch without a plan: tile ti of the tile map.
+__device__ __forceinline__ PrefillItem whole_tile(const int2* __restrict__ tiles, int ti,
+                                                  const int* __restrict__ cu,
+                                                  const int* __restrict__ seq_lens, int total_q,
+                                                  int rows_per_tile, int max_tokens, int window) {
+  PrefillItem it;
+  const int2 tl = tiles[ti];
+  const int2 rows = chunk_rows(cu, tl.x, total_q);
+  it.s = tl.x;
+  it.q0 = tl.y;
+  it.cu0 = rows.x;
+  it.n = rows.y - rows.x;
+  it.L = min(max(seq_lens[tl.x], 0), max_tokens);
+  const int last_pos = min(it.L - it.n + it.q0 + min(rows_per_tile, it.n - it.q0) - 1, it.L - 1);
+  it.i1 = last_pos >= 0 ? last_pos / kKeys + 1 : 0;
+  it.i0 = min(first_step(it.L - it.n + it.q0, window), it.i1);
+  it.slot = -1;
+  return it;
+}
+
 struct PrefillPlan {
   int items, splits, row_splits, pad;
 };

@@ -1,0 +1,73 @@
+// Chunked prefill with scores that are capped, biased by distance or cut to a window.
+
+#pragma once
+
+#include "prefill_tile.hpp"
+#include "scoring.hpp"
+
+namespace kvattn {
+
+__device__ __forceinline__ int first_lane(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// One workgroup per (item of the plan, or tile of the tile map without one; kv
+// head). kRows: the plan may hold one-row sequences.
+template <int G, bool kPow2Blocks, bool kRows, Cap kCap>
+__global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads),
+                          amdgpu_waves_per_eu(2, 2)))
+void scored_prompt_kernel(const uint16_t* __restrict__ q, const uint8_t* __restrict__ kv,
+                          int num_blocks, const int* __restrict__ block_table,
+                          const int* __restrict__ seq_lens, const int* __restrict__ cu,
+                          uint16_t* __restrict__ out, PrefillLaunch l, int total_q,
+                          int num_q_heads, int num_kv_heads, int max_blocks, int max_seq_len,
+                          ModScore<kCap> score) {
+  const int g = blockIdx.x % num_kv_heads;
+  const int ti = blockIdx.x / num_kv_heads;
+  PrefillItem it;
+  if (kRows || l.head) {
+    it = l.items[ti];   // the list has room for the whole grid: read beside the count
+    if (ti >= l.head->items) return;
+    // the same in every lane, which a load through a member of l does not tell the compiler
+    it = {first_lane(it.s), first_lane(it.q0), first_lane(it.i0), first_lane(it.i1),
+          first_lane(it.slot), first_lane(it.cu0), first_lane(it.n), first_lane(it.L)};
+  } else {              // no plan: the tile map's whole tiles
+    if (ti >= *l.tile_count) return;
+    it = whole_tile(l.tiles, ti, cu, seq_lens, total_q, 32 * kWaves / G,
+                    min(max_seq_len, max_blocks * kBS), score.window);
+  }
+  if (kRows && it.q0 < 0)
+    prefill_row<G>(it, g, q, kv, num_blocks, block_table, out, l.row_slots, num_q_heads,
+                   num_kv_heads, max_blocks, score);
+  else
+    prefill_tile<G, kPow2Blocks>(it, g, q, kv, num_blocks, block_table, out, l.slots, num_q_heads,
+                                 num_kv_heads, max_blocks, score);
+}
+
+template <int G, Cap kCap>
+static hipError_t launch_prefill_scored_t(const PrefillArgs& a, const PrefillLaunch& l) {
+  const bool rows = l.head && (a.num_seqs > 1 || a.total_q_tokens == 1);
+  const bool pow2 = (a.num_kv_heads & (a.num_kv_heads - 1)) == 0;
+  auto kernel = pow2 ? (rows ? scored_prompt_kernel<G, true, true, kCap>
+                             : scored_prompt_kernel<G, true, false, kCap>)
+                     : (rows ? scored_prompt_kernel<G, false, true, kCap>
+                             : scored_prompt_kernel<G, false, false, kCap>);
+  hipLaunchKernelGGL(kernel, dim3(l.blocks), dim3(kThreads), 0, a.stream,
+                     static_cast<const uint16_t*>(a.q), static_cast<const uint8_t*>(a.kv),
+                     a.num_blocks, a.block_table, a.seq_lens, a.cu_seqlens_q,
+                     static_cast<uint16_t*>(a.out), l, a.total_q_tokens, a.num_q_heads,
+                     a.num_kv_heads, a.max_blocks, a.max_seq_len,
+                     mod_score<kCap>(a.scale, *a.mods));
+  return hipGetLastError();
+}
+
+template <Cap kCap>
+static hipError_t dispatch_prefill_scored(const PrefillArgs& a, const PrefillLaunch& l) {
+  switch (a.num_q_heads / a.num_kv_heads) {
+    case 1: return launch_prefill_scored_t<1, kCap>(a, l);
+    case 2: return launch_prefill_scored_t<2, kCap>(a, l);
+    case 4: return launch_prefill_scored_t<4, kCap>(a, l);
+    case 8: return launch_prefill_scored_t<8, kCap>(a, l);
+    default: return hipErrorNotSupported;
+  }
+}
+
+}  // namespace kvattn

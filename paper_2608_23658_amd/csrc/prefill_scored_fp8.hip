@@ -1,0 +1,14 @@
+// Chunked prefill over a cache in 8 bits with scores that are capped, biased by distance or
+// cut to a window.
+
+#include "prefill_tile_fp8.hpp"
+
+namespace kvattn {
+
+hipError_t launch_prefill_scored_fp8(const PrefillArgs& a, const PrefillLaunch& l) {
+  return a.mods->softcap > 0.f
+             ? dispatch_prefill_fp8(a, l, mod_score<Cap::kYes>(a.scale, *a.mods))
+             : dispatch_prefill_fp8(a, l, mod_score<Cap::kNo>(a.scale, *a.mods));
+}
+
+}  // namespace kvattn

@@ -99,6 +99,9 @@ def lib() -> ctypes.CDLL:
     _c(L.kvattn_prefill_chunk_fp8, i32, vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32,
        i32, i32, i32, f32, i32, vp, sz, vp)
     sc = ctypes.POINTER(Scoring)
+    for f in (L.kvattn_prefill_chunk_scored, L.kvattn_prefill_chunk_scored_fp8):
+        _c(f, i32, vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, i32, i32, f32, sc,
+           i32, vp, sz, vp)
     for f in (L.kvattn_decode_scored, L.kvattn_decode_scored_fp8):
         _c(f, i32, vp, vp, i32, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, f32, sc, i32, vp, sz,
            vp)
@@ -571,6 +574,61 @@ def decode_scored_fp8(q: torch.Tensor, kv_layer, num_blocks: int, block_table: t
     return _decode_scored(lib().kvattn_decode_scored_fp8, q, kv_layer, num_blocks, block_table,
                           seq_lens, num_kv_heads, max_seq_len, softcap, slopes, window, block_size,
                           scale, out, ws, stream)
+
+
+def _prefill_scored(call, q, kv_layer, num_blocks, block_table, seq_lens, cu_seqlens_q,
+                    num_kv_heads, max_seq_len, max_num_batched_tokens, softcap, slopes, window,
+                    block_size, scale, out, ws, stream):
+    T, Hq, d = q.shape
+    _require_int32(block_table=block_table, seq_lens=seq_lens, cu_seqlens_q=cu_seqlens_q)
+    B = int(seq_lens.shape[0])
+    _require_rows(B, block_table, seq_lens, cu_seqlens_q)
+    _require_out(out, q)
+    code = _dtype_code(q.dtype)
+    scoring = _scoring(softcap, slopes, window, Hq)
+    _require_here(q, kv_layer, block_table, seq_lens, cu_seqlens_q, slopes, out, ws)
+    if out is None:
+        out = _made_for(stream, torch.empty_like, q, returned=True)
+    if ws is None:
+        ws = _made_for(stream, workspace, prefill_workspace_bytes(B, T, Hq, d), q.device)
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    budget = T if max_num_batched_tokens is None else int(max_num_batched_tokens)
+    check(call(q.data_ptr(), _ptr(kv_layer), int(num_blocks), block_table.data_ptr(),
+               seq_lens.data_ptr(), cu_seqlens_q.data_ptr(), out.data_ptr(), B, T, budget, Hq,
+               int(num_kv_heads), d, int(block_size), int(block_table.shape[1]), int(max_seq_len),
+               float(scale), scoring, code, ws.data_ptr(), ws.numel(), _stream(stream)))
+    return out
+
+
+def prefill_chunk_scored(q: torch.Tensor, kv_layer, num_blocks: int, block_table: torch.Tensor,
+                         seq_lens: torch.Tensor, cu_seqlens_q: torch.Tensor, *, num_kv_heads: int,
+                         max_seq_len: int, max_num_batched_tokens: Optional[int] = None,
+                         softcap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+                         window: int = 0, block_size: int = 16, scale: Optional[float] = None,
+                         out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                         stream=None) -> torch.Tensor:
+    """``prefill_chunk`` with the scores of ``decode_scored``: ``q`` [T, Hq, d] bf16."""
+    _require_layer(kv_layer, num_blocks, num_kv_heads, q.shape[2], q.element_size())
+    return _prefill_scored(lib().kvattn_prefill_chunk_scored, q, kv_layer, num_blocks, block_table,
+                           seq_lens, cu_seqlens_q, num_kv_heads, max_seq_len,
+                           max_num_batched_tokens, softcap, slopes, window, block_size, scale, out,
+                           ws, stream)
+
+
+def prefill_chunk_scored_fp8(q: torch.Tensor, kv_layer, num_blocks: int,
+                             block_table: torch.Tensor, seq_lens: torch.Tensor,
+                             cu_seqlens_q: torch.Tensor, *, num_kv_heads: int, max_seq_len: int,
+                             max_num_batched_tokens: Optional[int] = None, softcap: float = 0.0,
+                             slopes: Optional[torch.Tensor] = None, window: int = 0,
+                             block_size: int = 16, scale: Optional[float] = None,
+                             out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                             stream=None) -> torch.Tensor:
+    """``prefill_chunk_scored`` over a layer in 8 bits."""
+    _require_fp8_layer(kv_layer, num_blocks, num_kv_heads, q.shape[2])
+    return _prefill_scored(lib().kvattn_prefill_chunk_scored_fp8, q, kv_layer, num_blocks,
+                           block_table, seq_lens, cu_seqlens_q, num_kv_heads, max_seq_len,
+                           max_num_batched_tokens, softcap, slopes, window, block_size, scale, out,
+                           ws, stream)
 
 
 def _qkv_append(call, q, k, v, slot_mapping, kv_layer, num_blocks, positions, rope_table,

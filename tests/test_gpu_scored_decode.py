@@ -177,8 +177,9 @@ def test_streams_and_graphs():
     want = c.decode()
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
-    assert torch.equal(want, c.decode(stream=side))
+    got = c.decode(stream=side)
     torch.cuda.synchronize()
+    assert torch.equal(want, got)
     kw = dict(out=torch.empty_like(c.q), ws=K.workspace(K.decode_workspace_bytes(4, 8, 128, 715)),
               max_seq_len=2048)
     c.decode(**kw)
