@@ -25,7 +25,8 @@ SOURCES = ["abi.cpp", "kvpool.cpp", "blockpool.cpp", "decode.hip", "prefill.hip"
            "blocks.hip", "probes.hip",
            "append_fp8.hip", "prefill_fp8.hip", "step_map.hip", "qkv_append.hip",
            "qkv_append_fp8.hip", "decode_scored.hip",
-           "prefill_scored.hip", "prefill_capped.hip", "prefill_scored_fp8.hip"]
+           "prefill_scored.hip", "prefill_capped.hip",
+           "prefill_biased.hip", "prefill_scored_fp8.hip"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", "-Werror=inline-asm",
           "-I", INCLUDE, "-I", CSRC]

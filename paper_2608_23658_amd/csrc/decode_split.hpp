@@ -665,8 +665,8 @@ __global__ __launch_bounds__(kCombineWaves * kWave) void decode_combine_kernel(
 
 // The most tokens a call walks of a sequence: a window's, and those before it in its block.
 inline int most_tokens(const DecodeArgs& a, const PlainScore&) { return a.max_seq_len; }
-template <Cap kCap>
-int most_tokens(const DecodeArgs& a, const ModScore<kCap>& s) {
+template <Form kForm>
+int most_tokens(const DecodeArgs& a, const ModScore<kForm>& s) {
   return std::min(a.max_seq_len, s.window + 15);
 }
 

@@ -143,7 +143,8 @@ struct PrefillLaunch {
 };
 hipError_t launch_prefill_fp8(const PrefillArgs& a, const PrefillLaunch& l);
 hipError_t launch_prefill_scored(const PrefillArgs& a, const PrefillLaunch& l);
-hipError_t launch_prefill_capped(const PrefillArgs& a, const PrefillLaunch& l);   // of those
+hipError_t launch_prefill_capped(const PrefillArgs& a, const PrefillLaunch& l);
+hipError_t launch_prefill_biased(const PrefillArgs& a, const PrefillLaunch& l);
 hipError_t launch_prefill_scored_fp8(const PrefillArgs& a, const PrefillLaunch& l);
 
 // Workspace of a planned prefill step, whatever its kv head count.

@@ -5,7 +5,7 @@
 namespace kvattn {
 
 hipError_t launch_prefill_capped(const PrefillArgs& a, const PrefillLaunch& l) {
-  return dispatch_prefill_scored<Cap::kYes>(a, l);
+  return dispatch_prefill_scored<Form::kCap>(a, l);
 }
 
 }  // namespace kvattn

@@ -11,7 +11,7 @@ __device__ __forceinline__ int first_lane(int x) { return __builtin_amdgcn_readf
 
 // One workgroup per (item of the plan, or tile of the tile map without one; kv
 // head). kRows: the plan may hold one-row sequences.
-template <int G, bool kPow2Blocks, bool kRows, Cap kCap>
+template <int G, bool kPow2Blocks, bool kRows, Form kForm>
 __global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads),
                           amdgpu_waves_per_eu(2, 2)))
 void scored_prompt_kernel(const uint16_t* __restrict__ q, const uint8_t* __restrict__ kv,
@@ -19,7 +19,7 @@ void scored_prompt_kernel(const uint16_t* __restrict__ q, const uint8_t* __restr
                           const int* __restrict__ seq_lens, const int* __restrict__ cu,
                           uint16_t* __restrict__ out, PrefillLaunch l, int total_q,
                           int num_q_heads, int num_kv_heads, int max_blocks, int max_seq_len,
-                          ModScore<kCap> score) {
+                          ModScore<kForm> score) {
   const int g = blockIdx.x % num_kv_heads;
   const int ti = blockIdx.x / num_kv_heads;
   PrefillItem it;
@@ -42,30 +42,30 @@ void scored_prompt_kernel(const uint16_t* __restrict__ q, const uint8_t* __restr
                                  num_kv_heads, max_blocks, score);
 }
 
-template <int G, Cap kCap>
+template <int G, Form kForm>
 static hipError_t launch_prefill_scored_t(const PrefillArgs& a, const PrefillLaunch& l) {
   const bool rows = l.head && (a.num_seqs > 1 || a.total_q_tokens == 1);
   const bool pow2 = (a.num_kv_heads & (a.num_kv_heads - 1)) == 0;
-  auto kernel = pow2 ? (rows ? scored_prompt_kernel<G, true, true, kCap>
-                             : scored_prompt_kernel<G, true, false, kCap>)
-                     : (rows ? scored_prompt_kernel<G, false, true, kCap>
-                             : scored_prompt_kernel<G, false, false, kCap>);
+  auto kernel = pow2 ? (rows ? scored_prompt_kernel<G, true, true, kForm>
+                             : scored_prompt_kernel<G, true, false, kForm>)
+                     : (rows ? scored_prompt_kernel<G, false, true, kForm>
+                             : scored_prompt_kernel<G, false, false, kForm>);
   hipLaunchKernelGGL(kernel, dim3(l.blocks), dim3(kThreads), 0, a.stream,
                      static_cast<const uint16_t*>(a.q), static_cast<const uint8_t*>(a.kv),
                      a.num_blocks, a.block_table, a.seq_lens, a.cu_seqlens_q,
                      static_cast<uint16_t*>(a.out), l, a.total_q_tokens, a.num_q_heads,
                      a.num_kv_heads, a.max_blocks, a.max_seq_len,
-                     mod_score<kCap>(a.scale, *a.mods));
+                     mod_score<kForm>(a.scale, *a.mods));
   return hipGetLastError();
 }
 
-template <Cap kCap>
+template <Form kForm>
 static hipError_t dispatch_prefill_scored(const PrefillArgs& a, const PrefillLaunch& l) {
   switch (a.num_q_heads / a.num_kv_heads) {
-    case 1: return launch_prefill_scored_t<1, kCap>(a, l);
-    case 2: return launch_prefill_scored_t<2, kCap>(a, l);
-    case 4: return launch_prefill_scored_t<4, kCap>(a, l);
-    case 8: return launch_prefill_scored_t<8, kCap>(a, l);
+    case 1: return launch_prefill_scored_t<1, kForm>(a, l);
+    case 2: return launch_prefill_scored_t<2, kForm>(a, l);
+    case 4: return launch_prefill_scored_t<4, kForm>(a, l);
+    case 8: return launch_prefill_scored_t<8, kForm>(a, l);
     default: return hipErrorNotSupported;
   }
 }

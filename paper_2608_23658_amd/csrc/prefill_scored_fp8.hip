@@ -6,9 +6,8 @@
 namespace kvattn {
 
 hipError_t launch_prefill_scored_fp8(const PrefillArgs& a, const PrefillLaunch& l) {
-  return a.mods->softcap > 0.f
-             ? dispatch_prefill_fp8(a, l, mod_score<Cap::kYes>(a.scale, *a.mods))
-             : dispatch_prefill_fp8(a, l, mod_score<Cap::kNo>(a.scale, *a.mods));
+  return with_form(a.scale, *a.mods,
+                   [&](const auto& score) { return dispatch_prefill_fp8(a, l, score); });
 }
 
 }  // namespace kvattn

@@ -91,13 +91,11 @@ __device__ __forceinline__ void prefill_tile(
     if (tid == 0)
       lds_end = {out + (size_t)g * G * kD, slots + (size_t)g * kSlotBytes, it.slot, cu0, n,
                  num_q_heads * kD, num_kv_heads};
-  // what a step's scores are multiplied by on their way into the exponential
-  float exp_scale = score.scale_log2, slope = 0.f;
-  int work = 0;
+  float slope = 0.f;
+  __shared__ float lds_slope[kWaves];   // with a cap, which leaves no register for it
   if constexpr (Score::kOn) {
     slope = score.slope(h);
-    work = __builtin_amdgcn_readfirstlane(score.work(slope));
-    if (work) exp_scale = 1.f;
+    if (Score::form == Form::kCap && lane == 0) lds_slope[wave] = slope;
   }
 
   __shared__ __attribute__((aligned(16))) uint8_t lds_k[kKBufs][kStepBlocks][kTileBytes];
@@ -304,7 +302,7 @@ __device__ __forceinline__ void prefill_tile(
   };
   // Causal / length / real-block mask of one step's scores, in place; run
   // only on the steps that need it.
-  auto mask_scores = [&](int step, int bits, f32x16_t (&sr)[2]) {
+  auto mask_scores = [&](int step, int bits, f32x16_t (&sr)[2], float to) {
     const int kbase = step * kKeys;
     const int ln = lane_id_fresh();   // as in patch_v
     const int qpos = wave_pos0 + ln % 32;
@@ -316,7 +314,9 @@ __device__ __forceinline__ void prefill_tile(
         const int blk_ok = (bits >> (2 * kt + i / 8)) & 1;
         int keep = (kpos <= qpos) & (kpos < L) & blk_ok;
         if constexpr (Score::kOn) keep &= kpos > qpos - score.window;
-        sr[kt][i] = keep ? sr[kt][i] : -INFINITY;
+        sr[kt][i] = keep ? sr[kt][i] : to;
+        if constexpr (Score::kOn)   // a few comparisons' masks at a time
+          if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
   };
   auto needs_mask = [&](int step, int bits) __attribute__((always_inline)) {
@@ -362,8 +362,25 @@ __device__ __forceinline__ void prefill_tile(
     __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
     if (kPV && !step_clean(i - 1, bitsm1)) patch_v(i - 1, bitsm1);
     const bool do_k = i + 3 < N, do_v = i + 1 < N;
-    if constexpr (Score::kOn) score.apply(work, s_cur, i * kKeys - wave_pos0, slope, lane_id_fresh());
-    if (needs_mask(i, bits0)) mask_scores(i, bits0, s_cur);
+    const bool masked = needs_mask(i, bits0);
+    if constexpr (Score::form == Form::kCap)   // what a row does not see chooses no formula
+      if (masked) mask_scores(i, bits0, s_cur, 0.f);
+    const auto how = [&]() __attribute__((always_inline)) {
+      if constexpr (Score::kOn)
+        return score.prepare(s_cur, i * kKeys - wave_pos0,
+                             Score::form == Form::kCap ? lds_slope[wave] : slope,
+                             lane_id_fresh());
+      else
+        return score.scale_log2;
+    }();
+    // score e with a reference taken off
+    auto less = [&](int e, float r) __attribute__((always_inline)) {
+      if constexpr (Score::kOn)
+        return how.at(s_cur[e / 16][e % 16], e, r);
+      else
+        return fmaf(s_cur[e / 16][e % 16], how, -r);
+    };
+    if (masked) mask_scores(i, bits0, s_cur, -INFINITY);
 
     const int vbuf = (i + kVBufs - 1) % kVBufs;   // V of step i - 1
     const int kbuf = (i + 1) % kKBufs;            // K of step i + 1
@@ -409,7 +426,7 @@ __device__ __forceinline__ void prefill_tile(
       // current reference
       {
         const int e = k;
-        pe[e] = fast_exp2(fmaf(s_cur[e / 16][e % 16], exp_scale, -ref));
+        pe[e] = fast_exp2(less(e, ref));
         if (e % 2 == 1) {
           // the row sum adds the bf16 values that p.v multiplies
           pw[e / 2] = pack_bf16x2(pe[e - 1], pe[e]);
@@ -432,6 +449,18 @@ __device__ __forceinline__ void prefill_tile(
     // redo the step's exponentials against it. Rows that did not outgrow
     // theirs get the same values again.
     if (__builtin_amdgcn_ballot_w64(m_ref == -INFINITY || !(psum <= kPsumBound)) != 0) {
+      if constexpr (Score::kOn)   // finished, as the maximum needs them
+        if constexpr (Score::form == Form::kBias) {
+          // computed again here, not kept from the slots
+          asm volatile("" : "+v"(s_cur[0]), "+v"(s_cur[1]));
+#pragma unroll
+          for (int e = 0; e < 32; ++e) s_cur[e / 16][e % 16] = less(e, 0.f);
+        }
+      auto of_finished = [&](float x, float r) __attribute__((always_inline)) {
+        if constexpr (!Score::kOn) return fmaf(x, how, -r);
+        else if constexpr (Score::form == Form::kBias) return x - r;
+        else return fmaf(x, how.by, -r);
+      };
       float mp0 = -INFINITY, mp1 = -INFINITY;
 #pragma unroll
       for (int e = 0; e < 32; e += 4) {
@@ -440,7 +469,7 @@ __device__ __forceinline__ void prefill_tile(
       }
       float mx = max3f(mp0, mp1, mp1);
       mx = max3f(mx, __shfl_xor(mx, 32, kWave), mx);
-      const float tmax = mx * exp_scale;
+      const float tmax = of_finished(mx, 0.f);
       const bool grow = tmax > m_ref + kLazyRescale;
       rescale = __builtin_amdgcn_ballot_w64(grow) != 0;
       const float nref = grow ? tmax : m_ref;
@@ -450,8 +479,8 @@ __device__ __forceinline__ void prefill_tile(
       psum = 0.f;
 #pragma unroll
       for (int e = 0; e < 32; e += 2) {
-        pw[e / 2] = pack_bf16x2(fast_exp2(fmaf(s_cur[e / 16][e % 16], exp_scale, -ref)),
-                                fast_exp2(fmaf(s_cur[e / 16][e % 16 + 1], exp_scale, -ref)));
+        pw[e / 2] = pack_bf16x2(fast_exp2(of_finished(s_cur[e / 16][e % 16], ref)),
+                                fast_exp2(of_finished(s_cur[e / 16][e % 16 + 1], ref)));
         psum = dot2_bf16(pw[e / 2], kBf16OnePair, psum);
       }
     }

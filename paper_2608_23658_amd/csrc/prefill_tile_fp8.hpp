@@ -65,13 +65,11 @@ __device__ __forceinline__ void prefill_tile_fp8(
   // first key that any row of the tile sees
   int lo = 0;
   if constexpr (Score::kOn) lo = score.first_key(c + q0);
-  // what a step's scores are multiplied by on their way into the exponential
-  float exp_scale = score.scale_log2, slope = 0.f;
-  int work = 0;
+  float slope = 0.f;
+  __shared__ float lds_slope[kWaves];   // with a cap, which leaves no register for it
   if constexpr (Score::kOn) {
     slope = score.slope(h);
-    work = __builtin_amdgcn_readfirstlane(score.work(slope));
-    if (work) exp_scale = 1.f;
+    if (Score::form == Form::kCap && lane == 0) lds_slope[wave] = slope;
   }
 
   struct Lds {
@@ -266,7 +264,7 @@ __device__ __forceinline__ void prefill_tile_fp8(
   };
   // Causal / length / real-block mask of one step's scores, in place; run
   // only on the steps that need it.
-  auto mask_scores = [&](int step, int bits, f32x16_t (&sr)[2]) {
+  auto mask_scores = [&](int step, int bits, f32x16_t (&sr)[2], float to) {
     const int kbase = step * kKeys;
     const int ln = lane_id_fresh();
     const int qpos = wave_pos0 + ln % 32;
@@ -278,7 +276,9 @@ __device__ __forceinline__ void prefill_tile_fp8(
         const int blk_ok = (bits >> (2 * kt + i / 8)) & 1;
         int keep = (kpos <= qpos) & (kpos < L) & blk_ok;
         if constexpr (Score::kOn) keep &= kpos > qpos - score.window;
-        sr[kt][i] = keep ? sr[kt][i] : -INFINITY;
+        sr[kt][i] = keep ? sr[kt][i] : to;
+        if constexpr (Score::kOn)   // a few comparisons' masks at a time
+          if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
   };
   auto needs_mask = [&](int step, int bits) __attribute__((always_inline)) {
@@ -323,8 +323,25 @@ __device__ __forceinline__ void prefill_tile_fp8(
     // (scalar loads share the lgkm counter with LDS reads and return out of
     // order).
     __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
-    if constexpr (Score::kOn) score.apply(work, s_cur, i * kKeys - wave_pos0, slope, lane_id_fresh());
-    if (needs_mask(i, bits & 0xf)) mask_scores(i, bits & 0xf, s_cur);
+    const bool masked = needs_mask(i, bits & 0xf);
+    if constexpr (Score::form == Form::kCap)   // what a row does not see chooses no formula
+      if (masked) mask_scores(i, bits & 0xf, s_cur, 0.f);
+    const auto how = [&]() __attribute__((always_inline)) {
+      if constexpr (Score::kOn)
+        return score.prepare(s_cur, i * kKeys - wave_pos0,
+                             Score::form == Form::kCap ? lds_slope[wave] : slope,
+                             lane_id_fresh());
+      else
+        return score.scale_log2;
+    }();
+    // score e with a reference taken off
+    auto less = [&](int e, float r) __attribute__((always_inline)) {
+      if constexpr (Score::kOn)
+        return how.at(s_cur[e / 16][e % 16], e, r);
+      else
+        return fmaf(s_cur[e / 16][e % 16], how, -r);
+    };
+    if (masked) mask_scores(i, bits & 0xf, s_cur, -INFINITY);
     // here and not where it is converted, so that no branch splits the slots
     if (v_masked(i, v_id)) v_patch(i, v_id);
 
@@ -371,7 +388,7 @@ __device__ __forceinline__ void prefill_tile_fp8(
       // current reference
       {
         const int e = k;
-        pe[e] = fast_exp2(fmaf(s_cur[e / 16][e % 16], exp_scale, -ref));
+        pe[e] = fast_exp2(less(e, ref));
         if (e % 2 == 1) {
           // A weight is rounded to bf16, as the matrix instruction takes it (at most 2^-8
           // of it); the row sum adds the rounded ones, so that they add up to one.
@@ -395,6 +412,18 @@ __device__ __forceinline__ void prefill_tile_fp8(
     // redo the step's exponentials against it. Rows that did not outgrow
     // theirs get the same values again.
     if (__builtin_amdgcn_ballot_w64(m_ref == -INFINITY || !(psum <= kPsumBound)) != 0) {
+      if constexpr (Score::kOn)   // finished, as the maximum needs them
+        if constexpr (Score::form == Form::kBias) {
+          // computed again here, not kept from the slots
+          asm volatile("" : "+v"(s_cur[0]), "+v"(s_cur[1]));
+#pragma unroll
+          for (int e = 0; e < 32; ++e) s_cur[e / 16][e % 16] = less(e, 0.f);
+        }
+      auto of_finished = [&](float x, float r) __attribute__((always_inline)) {
+        if constexpr (!Score::kOn) return fmaf(x, how, -r);
+        else if constexpr (Score::form == Form::kBias) return x - r;
+        else return fmaf(x, how.by, -r);
+      };
       float mp0 = -INFINITY, mp1 = -INFINITY;
 #pragma unroll
       for (int e = 0; e < 32; e += 4) {
@@ -403,7 +432,7 @@ __device__ __forceinline__ void prefill_tile_fp8(
       }
       float mx = max3f(mp0, mp1, mp1);
       mx = max3f(mx, __shfl_xor(mx, 32, kWave), mx);
-      const float tmax = mx * exp_scale;
+      const float tmax = of_finished(mx, 0.f);
       const bool grow = tmax > m_ref + kLazyRescale;
       rescale = __builtin_amdgcn_ballot_w64(grow) != 0;
       const float nref = grow ? tmax : m_ref;
@@ -413,8 +442,8 @@ __device__ __forceinline__ void prefill_tile_fp8(
       psum = 0.f;
 #pragma unroll
       for (int e = 0; e < 32; e += 2) {
-        pw[e / 2] = pack_bf16x2(fast_exp2(fmaf(s_cur[e / 16][e % 16], exp_scale, -ref)),
-                                fast_exp2(fmaf(s_cur[e / 16][e % 16 + 1], exp_scale, -ref)));
+        pw[e / 2] = pack_bf16x2(fast_exp2(of_finished(s_cur[e / 16][e % 16], ref)),
+                                fast_exp2(of_finished(s_cur[e / 16][e % 16 + 1], ref)));
         psum = dot2_bf16(pw[e / 2], kBf16OnePair, psum);
       }
     }

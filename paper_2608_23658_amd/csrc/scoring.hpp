@@ -2,6 +2,8 @@
 // cut to a window.
 #pragma once
 
+#include <cmath>
+
 #include "common.hpp"
 #include "launch.hpp"
 
@@ -9,28 +11,41 @@ namespace kvattn {
 
 constexpr int kNoWindow = 0x3fffffff;
 
+// What the scores of a kernel can be; all but plain ones have a window. kAny asks for each
+// score.
+enum class Form { kPlain, kWindow, kBias, kCap, kAny };
+
 // scale * q . k, causal.
 struct PlainScore {
   static constexpr bool kOn = false;
+  static constexpr Form form = Form::kPlain;
   static constexpr int window = kNoWindow;
   float scale_log2;
   __device__ __forceinline__ const PlainScore& held() const { return *this; }
 };
 
+// The odd polynomials nearest to tanh in [0, 0.6] (off by 8e-8 of it) and [0, 0.5] (by 7e-7):
+// z + z^3 (c0 + c1 z^2 + ..).
+constexpr float kTanh4[4] = {-0.333326216f, 0.133135208f, -0.0522311078f, 0.0156404821f};
+constexpr float kTanh3[3] = {-0.333282646f, 0.132067148f, -0.0447894702f};
+
 // a = scale q.k; a = cap tanh(a / cap); a += slope (key - row); keys from row - window + 1 on.
 // All in the log2 domain.
-enum class Cap { kNo, kYes, kAsk };   // known where the kernel is built, or asked for each score
-template <Cap kCap>
+template <Form kForm>
 struct ModScore {
   static constexpr bool kOn = true;
+  static constexpr Form form = kForm;
   float scale_log2;       // of q . k
   float cap_log2;         // 0: no cap
   float tanh_scale;       // a / cap of a q . k
   const float* slopes;    // of every query head, null: no bias
   int window;             // kNoWindow: none
+  // With a cap, of products smaller than near: a score is dot (p0 + p1 dot^2 + p2 dot^4 +
+  // p3 dot^6), by kTanh3.
+  float near, p0, p1, p2, p3;
 
   __device__ __forceinline__ bool has_cap() const {
-    return kCap == Cap::kYes || (kCap == Cap::kAsk && cap_log2 > 0.f);
+    return kForm == Form::kCap || (kForm == Form::kAny && cap_log2 > 0.f);
   }
   __device__ __forceinline__ float slope(int head) const {
     return slopes ? slopes[head] * kLog2e : 0.f;
@@ -38,23 +53,31 @@ struct ModScore {
   // First key that the row at position pos sees.
   __device__ __forceinline__ int first_key(int pos) const { return max(0, pos - window + 1); }
 
-  // cap tanh(dot scale / cap). Near zero by the odd polynomial that is nearest to tanh in
-  // [0, 0.6], off by 8e-8 of it; from there on 1 - 2 / (e^2x + 1), whose error, 2^-22 of the
-  // cap, is then small beside the value. kExact: the library's tanh, for fp32.
+  // cap tanh(dot scale / cap) as cap (1 - 2 / (e^2x + 1)), off by 2^-22 of the cap, which for
+  // one up to kSmallCap is 2^-14 of a weight; for a larger one, near zero, by kTanh4. kExact:
+  // the library's tanh.
+  static constexpr float kSmallCap = 256.f;   // in the log2 domain
+  static __device__ __forceinline__ float capped_far(float z, float cap_log2) {
+    const float u = fast_exp2(z * (2.f * kLog2e));
+    return fmaf(-2.f * cap_log2, __builtin_amdgcn_rcpf(u + 1.f), cap_log2);
+  }
+  static __device__ __forceinline__ float capped_near(float z, float cap_log2) {
+    const float w = z * z;
+    float h = fmaf(w, kTanh4[3], kTanh4[2]);
+    h = fmaf(h, w, kTanh4[1]);
+    h = fmaf(h, w, kTanh4[0]);
+    return z * cap_log2 * fmaf(h, w, 1.f);
+  }
   template <bool kExact>
   __device__ __forceinline__ float capped(float dot) const {
     const float z = dot * tanh_scale;
     if constexpr (kExact) return cap_log2 * tanhf(z);
-    const float w = z * z;
-    float h = fmaf(w, kTanh[3], kTanh[2]);
-    h = fmaf(h, w, kTanh[1]);
-    h = fmaf(h, w, kTanh[0]);
-    const float near = dot * scale_log2 * fmaf(h, w, 1.f);
-    const float u = fast_exp2(z * (2.f * kLog2e));
-    const float far = fmaf(-2.f * cap_log2, __builtin_amdgcn_rcpf(u + 1.f), cap_log2);
-    return fabsf(z) < 0.6f ? near : far;
+    const float far = capped_far(z, cap_log2);
+    if (cap_log2 <= kSmallCap) return far;
+    return fabsf(z) < 0.6f ? capped_near(z, cap_log2) : far;
   }
-  static constexpr float kTanh[4] = {-0.333326216f, 0.133135208f, -0.0522311078f, 0.0156404821f};
+
+  // ---- for a walk, score by score ----
 
   // The same in vector registers: a walk's scalar ones are full of addresses.
   __device__ __forceinline__ ModScore held() const {
@@ -62,47 +85,93 @@ struct ModScore {
     asm("" : "+v"(s.scale_log2), "+v"(s.cap_log2), "+v"(s.tanh_scale));
     return s;
   }
-
-  // What a prefill tile does to its scores before its softmax (apply): nothing, and then
-  // they only miss their scale, which is above zero so that masked ones may be minus
-  // infinity; or all that makes them, for heads with a slope and without.
-  enum Work : int { kNothing, kScale, kBias };
-  __device__ __forceinline__ int work(float slope_log2) const {
-    return slope_log2 != 0.f ? kBias : kCap == Cap::kYes || !(scale_log2 > 0.f) ? kScale : kNothing;
-  }
-  // Finishes the scores of 64 keys and 32 rows as a prefill tile's lane holds them: element e
-  // of s[t] is key 32 t + 16 (e / 8) + 8 (lane / 32) + e % 8 of the step, whose first key is
-  // rel tokens after the wavefront's first row; the row is lane % 32.
-  template <typename V>
-  __device__ __forceinline__ void apply(int work, V (&s)[2], int rel, float slope_log2,
-                                        int lane) const {
-    asm volatile("" : "+s"(work));   // compared here each time, not kept as masks over the loop
-    if (kCap == Cap::kYes) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[t][e] = capped<false>(s[t][e]);
-    } else if (work != kNothing) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[t][e] *= scale_log2;
-    }
-    if (work == kBias) {
-      const float b = slope_log2 * (float)(rel + lane / 32 * 8 - lane % 32);
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          s[t][e] += fmaf(slope_log2, (float)(32 * t + e / 8 * 16 + e % 8), b);
-    }
-  }
-
   // The score of a key that lies ago tokens before the row.
   template <bool kExact>
   __device__ __forceinline__ float at(float dot, float slope_log2, int ago) const {
-    const float x = has_cap() ? capped<kExact>(dot) : dot * scale_log2;
+    const float x =
+        has_cap() ? capped<kExact>(dot) : dot * scale_log2;
     return fmaf(slope_log2, -(float)ago, x);
+  }
+
+  // ---- for a prefill tile, the scores of 64 keys and 32 rows at a time ----
+  // As a lane holds them: element e is key key_of(e) + 8 (lane / 32) of the step, whose first
+  // key is rel tokens after the wavefront's first row; the row is lane % 32.
+
+  static __device__ __forceinline__ constexpr int key_of(int e) {
+    return e / 16 * 32 + e / 8 % 2 * 16 + e % 8;
+  }
+  // How the softmax finds a step's scores, with its reference r taken off.
+  struct Step {
+    float by;               // times this
+    float slope, first;     // kBias: the bias of element e is slope key_of(e) + first
+    __device__ __forceinline__ float at(float dot, int e, float r) const {
+      if constexpr (kForm == Form::kBias)
+        return fmaf(dot, by, fmaf(slope, (float)key_of(e), first - r));
+      return fmaf(dot, by, -r);
+    }
+  };
+
+  // Values in vector registers from here on: not hoisted out of a tile's loop, which has none
+  // to spare.
+  static __device__ __forceinline__ void hold(float& x) { asm volatile("" : "+v"(x)); }
+  template <typename... T>
+  static __device__ __forceinline__ void here(T&... x) {
+    (hold(x), ...);
+  }
+  // Prepares a step's scores s, before they are masked: capped ones, and those of a scale that
+  // is not above zero, are finished; others the softmax finishes beside the matrix work.
+  template <typename V>
+  __device__ __forceinline__ Step prepare(V (&s)[2], int rel, const float& slope_log2,
+                                          int lane) const {
+    const float at_lane = (float)(rel + lane / 32 * 8 - lane % 32);
+    if constexpr (kForm == Form::kCap) {
+      if (all_near(s)) {
+        float c0 = p0, c1 = p1, c2 = p2, c3 = p3;
+        here(c0, c1, c2, c3);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const float x = s[e / 16][e % 16], t = x * x;
+          s[e / 16][e % 16] = x * fmaf(fmaf(fmaf(t, c3, c2), t, c1), t, c0);
+        }
+      } else {
+        float scale = tanh_scale, cap = cap_log2;
+        here(scale, cap);
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          s[e / 16][e % 16] = capped_far(s[e / 16][e % 16] * scale, cap);
+      }
+      const float slope =
+          __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(slope_log2)));
+      if (slope != 0.f) {
+        float at = at_lane, by = slope;
+        here(at, by);
+        const float first = by * at;
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          s[e / 16][e % 16] += fmaf(by, (float)key_of(e), first);
+      }
+      return {1.f, 0.f, 0.f};
+    } else {
+      const float first = slope_log2 * at_lane;
+      if (scale_log2 > 0.f) return {scale_log2, slope_log2, first};
+      // masked scores are minus infinity before a scale above zero
+#pragma unroll
+      for (int e = 0; e < 32; ++e) s[e / 16][e % 16] *= scale_log2;
+      return {1.f, slope_log2, first};
+    }
+  }
+  // Whether all of a wavefront's products are smaller than near.
+  template <typename V>
+  __device__ __forceinline__ bool all_near(const V (&s)[2]) const {
+    float m = 0.f;
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+      float r;
+      asm("v_max3_f32 %0, |%1|, |%2|, %3"
+          : "=v"(r) : "v"(s[e / 16][e % 16]), "v"(s[e / 16][e % 16 + 1]), "v"(m));
+      m = r;
+    }
+    return __builtin_amdgcn_ballot_w64(!(m < near)) == 0;
   }
 };
 
@@ -110,15 +179,30 @@ inline int window_keys(const ScoreMods& m) {
   return m.window > 0 && m.window < kNoWindow ? m.window : kNoWindow;
 }
 
-template <Cap kCap>
-ModScore<kCap> mod_score(float scale, const ScoreMods& m) {
-  ModScore<kCap> s;
+template <Form kForm>
+ModScore<kForm> mod_score(float scale, const ScoreMods& m) {
+  ModScore<kForm> s;
   s.scale_log2 = scale * kLog2e;
   s.cap_log2 = m.softcap * kLog2e;
   s.tanh_scale = m.softcap > 0.f ? scale / m.softcap : 0.f;
   s.slopes = m.slopes;
   s.window = window_keys(m);
+  const float w = s.tanh_scale * s.tanh_scale;
+  s.p0 = s.scale_log2;
+  s.p1 = s.p0 * w * kTanh3[0];
+  s.p2 = s.p0 * w * w * kTanh3[1];
+  s.p3 = s.p0 * w * w * w * kTanh3[2];
+  // none is near where a coefficient has left fp32's range (a tiny cap)
+  s.near = w < 1e9f && std::isfinite(s.p3) ? 0.5f / std::fabs(s.tanh_scale) : 0.f;
   return s;
+}
+
+// Calls launch with a call's scores in their form's type.
+template <typename Launch>
+hipError_t with_form(float scale, const ScoreMods& m, Launch launch) {
+  if (m.softcap > 0.f) return launch(mod_score<Form::kCap>(scale, m));
+  if (m.slopes) return launch(mod_score<Form::kBias>(scale, m));
+  return launch(mod_score<Form::kWindow>(scale, m));
 }
 
 }  // namespace kvattn
