@@ -81,6 +81,13 @@ __device__ __forceinline__ void prefill_tile(
   const int c = L - n;                          // cached context before the chunk
   const int i0 = it.i0, N = it.i1;              // steps of the item
   __builtin_assume(i0 >= 0 && N >= 0);
+  // The key step that is walked as step i. Biased scores grow towards a row's own key, by
+  // more than the softmax's reference allows in a step where the slope is steep: those are
+  // walked from the last keys to the first, so that the reference, once set, holds.
+  const int ends = i0 + N - 1;
+  auto at_step = [&](int i) __attribute__((always_inline)) {
+    return Score::form == Form::kBias || Score::form == Form::kCap ? ends - i : i;
+  };
   const bool idle = row0 >= n;                  // none of the wave's 32 rows is in the chunk
   // first key that any row of the tile sees
   int lo = 0;
@@ -153,7 +160,7 @@ __device__ __forceinline__ void prefill_tile(
   };
   auto step_ids = [&](int step) __attribute__((always_inline)) {
     StepIds r;
-    const int b0 = step * kStepBlocks;
+    const int b0 = at_step(step) * kStepBlocks;
     if (b0 + kStepBlocks <= nblk) {
       const i32x4_t v = scalar_entries4(bt, b0);
 #pragma unroll
@@ -223,7 +230,7 @@ __device__ __forceinline__ void prefill_tile(
   // identical and idempotent, so no barrier is needed between them. Called
   // only when such slots exist.
   auto patch_v = [&](int step, int bits) __attribute__((always_inline)) {
-    const int kbase = step * kKeys;
+    const int kbase = at_step(step) * kKeys;
     // recomputed here, so no lane constant of this rare path stays live
     // across the pipelined loop
     const int ln = lane_id_fresh();
@@ -258,7 +265,7 @@ __device__ __forceinline__ void prefill_tile(
       bits = __builtin_amdgcn_readfirstlane(bits);
       asm volatile("" : "+s"(bits));   // compared each time, no mask kept
     }
-    return bits == 0xf && (step + 1) * kKeys <= L && (!Score::kOn || step * kKeys >= lo);
+    return bits == 0xf && (at_step(step) + 1) * kKeys <= L && (!Score::kOn || at_step(step) * kKeys >= lo);
   };
 
   const int wave_pos0 = c + row0;   // position of the wave's first row
@@ -303,7 +310,7 @@ __device__ __forceinline__ void prefill_tile(
   // Causal / length / real-block mask of one step's scores, in place; run
   // only on the steps that need it.
   auto mask_scores = [&](int step, int bits, f32x16_t (&sr)[2], float to) {
-    const int kbase = step * kKeys;
+    const int kbase = at_step(step) * kKeys;
     const int ln = lane_id_fresh();   // as in patch_v
     const int qpos = wave_pos0 + ln % 32;
 #pragma unroll
@@ -320,8 +327,8 @@ __device__ __forceinline__ void prefill_tile(
       }
   };
   auto needs_mask = [&](int step, int bits) __attribute__((always_inline)) {
-    return (step * kKeys + kKeys - 1 > wave_pos0) || !step_clean(step, bits) ||
-           (Score::kOn && step * kKeys <= wave_pos0 + 31 - score.window);
+    return (at_step(step) * kKeys + kKeys - 1 > wave_pos0) || !step_clean(step, bits) ||
+           (Score::kOn && at_step(step) * kKeys <= wave_pos0 + 31 - score.window);
   };
   // bitsm1, bits0 .. bits3: real-block masks of steps i - 1, i .. i + 3
   int bitsm1 = 0, bits0 = 0, bits1 = 0, bits2 = 0, bits3 = 0;
@@ -367,7 +374,7 @@ __device__ __forceinline__ void prefill_tile(
       if (masked) mask_scores(i, bits0, s_cur, 0.f);
     const auto how = [&]() __attribute__((always_inline)) {
       if constexpr (Score::kOn)
-        return score.prepare(s_cur, i * kKeys - wave_pos0,
+        return score.prepare(s_cur, at_step(i) * kKeys - wave_pos0,
                              Score::form == Form::kCap ? lds_slope[wave] : slope,
                              lane_id_fresh());
       else

@@ -61,6 +61,13 @@ __device__ __forceinline__ void prefill_tile_fp8(
   const int c = L - n;                          // cached context before the chunk
   const int i0 = it.i0, N = it.i1;              // steps of the item
   __builtin_assume(i0 >= 0 && N >= 0);
+  // The key step that is walked as step i. Biased scores grow towards a row's own key, by
+  // more than the softmax's reference allows in a step where the slope is steep: those are
+  // walked from the last keys to the first, so that the reference, once set, holds.
+  const int ends = i0 + N - 1;
+  auto at_step = [&](int i) __attribute__((always_inline)) {
+    return Score::form == Form::kBias || Score::form == Form::kCap ? ends - i : i;
+  };
   const bool idle = row0 >= n;                  // none of the wave's 32 rows is in the chunk
   // first key that any row of the tile sees
   int lo = 0;
@@ -133,7 +140,7 @@ __device__ __forceinline__ void prefill_tile_fp8(
   };
   auto step_ids = [&](int step) __attribute__((always_inline)) {
     StepIds r;
-    const int b0 = step * kStepBlocks;
+    const int b0 = at_step(step) * kStepBlocks;
     if (b0 + kStepBlocks <= nblk) {
       const i32x4_t v = scalar_entries4(bt, b0);
 #pragma unroll
@@ -159,7 +166,7 @@ __device__ __forceinline__ void prefill_tile_fp8(
   const int my_kb = wave / 2, my_half = wave % 2;
   // This wavefront's block of a step alone, and an id as it counts.
   auto my_entry = [&](int step) __attribute__((always_inline)) {
-    const int b = step * kStepBlocks + my_kb;
+    const int b = at_step(step) * kStepBlocks + my_kb;
     return b < nblk ? scalar_entry(bt, b) : -1;
   };
   auto real = [&](int id) __attribute__((always_inline)) { return real_id(id) ? id : -1; };
@@ -196,12 +203,12 @@ __device__ __forceinline__ void prefill_tile_fp8(
   };
   // Whether this wavefront's V block of a step holds slots that must not contribute.
   auto v_masked = [&](int step, int id) __attribute__((always_inline)) {
-    return id < 0 || step * kKeys + (my_kb + 1) * kBS > L ||
-           (Score::kOn && step * kKeys + my_kb * kBS < lo);
+    return id < 0 || at_step(step) * kKeys + (my_kb + 1) * kBS > L ||
+           (Score::kOn && at_step(step) * kKeys + my_kb * kBS < lo);
   };
   auto v_patch = [&](int step, int id) __attribute__((always_inline)) {
     const unsigned ln = lane_id_fresh();
-    const int key = step * kKeys + my_kb * kBS + (int)(ln / 16) * 4;
+    const int key = at_step(step) * kKeys + my_kb * kBS + (int)(ln / 16) * 4;
     uint32_t keep = id < 0 ? 0u : first_bytes(L - key);
     if constexpr (Score::kOn) keep &= ~first_bytes(lo - key);
     rv = make_uint4(rv.x & keep, rv.y & keep, rv.z & keep, rv.w & keep);
@@ -220,7 +227,7 @@ __device__ __forceinline__ void prefill_tile_fp8(
     put_v(buf, v_at, 3, rv.w, v_scale(exps));
   };
   auto step_clean = [&](int step, int bits) __attribute__((always_inline)) {
-    return bits == 0xf && (step + 1) * kKeys <= L;
+    return bits == 0xf && (at_step(step) + 1) * kKeys <= L;
   };
 
   const int wave_pos0 = c + row0;   // position of the wave's first row
@@ -265,7 +272,7 @@ __device__ __forceinline__ void prefill_tile_fp8(
   // Causal / length / real-block mask of one step's scores, in place; run
   // only on the steps that need it.
   auto mask_scores = [&](int step, int bits, f32x16_t (&sr)[2], float to) {
-    const int kbase = step * kKeys;
+    const int kbase = at_step(step) * kKeys;
     const int ln = lane_id_fresh();
     const int qpos = wave_pos0 + ln % 32;
 #pragma unroll
@@ -282,8 +289,8 @@ __device__ __forceinline__ void prefill_tile_fp8(
       }
   };
   auto needs_mask = [&](int step, int bits) __attribute__((always_inline)) {
-    return (step * kKeys + kKeys - 1 > wave_pos0) || !step_clean(step, bits) ||
-           (Score::kOn && step * kKeys <= wave_pos0 + 31 - score.window);
+    return (at_step(step) * kKeys + kKeys - 1 > wave_pos0) || !step_clean(step, bits) ||
+           (Score::kOn && at_step(step) * kKeys <= wave_pos0 + 31 - score.window);
   };
   // real-block masks of steps i .. i + 3, four bits each
   int bits = 0;
@@ -328,7 +335,7 @@ __device__ __forceinline__ void prefill_tile_fp8(
       if (masked) mask_scores(i, bits & 0xf, s_cur, 0.f);
     const auto how = [&]() __attribute__((always_inline)) {
       if constexpr (Score::kOn)
-        return score.prepare(s_cur, i * kKeys - wave_pos0,
+        return score.prepare(s_cur, at_step(i) * kKeys - wave_pos0,
                              Score::form == Form::kCap ? lds_slope[wave] : slope,
                              lane_id_fresh());
       else
