@@ -229,12 +229,14 @@ __device__ __forceinline__ void walk_f32(const DecodeTiles<false>& tiles, const 
 #pragma unroll
     for (int h = 0; h < G; ++h) {
       float x;
-      if constexpr (Score::kOn)
-        x = kvalid && tb + lane >= lo
-                ? score.template at<true>(sc[h], slope[h], own - (tb + lane))
-                : -INFINITY;
-      else
+      if constexpr (Score::kOn) {
+        float one[1] = {sc[h]};
+        score.template cap<true>(one);
+        x = kvalid && tb + lane >= lo ? fmaf(slope[h], -(float)(own - (tb + lane)), one[0])
+                                      : -INFINITY;
+      } else {
         x = kvalid ? sc[h] * score.scale_log2 : -INFINITY;
+      }
       const float mn = fmaxf(m_run[h], wave_max(x));
       const float ref = (mn == -INFINITY) ? 0.f : mn;
       alpha[h] = fast_exp2(m_run[h] - ref);

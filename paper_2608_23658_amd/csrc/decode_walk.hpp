@@ -153,6 +153,26 @@ __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
   // lane's 16 bytes of a V KiB (32 dims x 2 halves): dim l % 32, half l / 32
   const int v_lane = 2 * (lane % 32) + lane / 32;
 
+  // Zeroes V's slots at or past t1, or before lo: they may hold anything, and zero times NaN
+  // is NaN.
+  auto cut = [&](int tb, uint4 (&vreg)[S::kTB][S::kVI]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < S::kTB; ++j) {
+      const int tok = tb + j * S::kBS + (lane / 32) * 8;
+      auto seen = [&](int t) { return t < t1 && (!Score::kOn || t >= lo); };
+#pragma unroll
+      for (int i = 0; i < S::kVI; ++i) {
+        uint32_t w[4] = {vreg[j][i].x, vreg[j][i].y, vreg[j][i].z, vreg[j][i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t lo16 = seen(tok + 2 * k) ? 0x0000ffffu : 0u;
+          const uint32_t hi16 = seen(tok + 2 * k + 1) ? 0xffff0000u : 0u;
+          w[k] &= (lo16 | hi16);
+        }
+        vreg[j][i] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  };
   // The products and softmax of one loaded step; tail: it may end inside a
   // block; zero: a block without a valid id still holds what was loaded for it.
   auto compute = [&](int tb, const int (&bid)[S::kTB], bool tail, bool zero,
@@ -168,13 +188,22 @@ __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
         sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kreg[j][i]),
                                                      __builtin_bit_cast(bf16x8_t, qreg[i]), sc, 0,
                                                      0, 0);
+      if constexpr (Score::kOn) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[j][r] = sc[r];
+        score.template cap<false>(x[j]);
+        if (score.slopes) {
+          const float far = (float)(own - (tb + j * S::kBS + row * 4));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[j][r] = fmaf(slope, (float)r - far, x[j][r]);
+        }
+      }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int tok = tb + j * S::kBS + row * 4 + r;
         const bool keep = bid[j] >= 0 && (!tail || tok < t1);
         if constexpr (Score::kOn)
-          x[j][r] = keep && tok >= lo ? score.template at<false>(sc[r], slope, own - tok)
-                                      : -INFINITY;
+          x[j][r] = keep && tok >= lo ? x[j][r] : -INFINITY;
         else
           x[j][r] = keep ? sc[r] * score.scale_log2 : -INFINITY;
       }
@@ -213,25 +242,7 @@ __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
         for (int i = 0; i < S::kVI; ++i) vreg[j][i] = make_uint4(0, 0, 0, 0);
       }
     }
-    if (tail || (Score::kOn && tb < lo)) {
-#pragma unroll
-      for (int j = 0; j < S::kTB; ++j) {
-        // slots at or past t1 (or before lo) may hold anything, and zero times NaN is NaN
-        const int tok = tb + j * S::kBS + (lane / 32) * 8;
-        auto seen = [&](int t) { return t < t1 && (!Score::kOn || t >= lo); };
-#pragma unroll
-        for (int i = 0; i < S::kVI; ++i) {
-          uint32_t w[4] = {vreg[j][i].x, vreg[j][i].y, vreg[j][i].z, vreg[j][i].w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t lo16 = seen(tok + 2 * k) ? 0x0000ffffu : 0u;
-            const uint32_t hi16 = seen(tok + 2 * k + 1) ? 0xffff0000u : 0u;
-            w[k] &= (lo16 | hi16);
-          }
-          vreg[j][i] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-      }
-    }
+    if (tail || (Score::kOn && !kAhead && tb < lo)) cut(tb, vreg);
 #pragma unroll
     for (int j = 0; j < S::kTB; j += 2) {
       uint2 p0 = pw[j], p1 = pw[j + 1];
@@ -273,6 +284,9 @@ __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
     int tb = t0;
     step_ids(tb, id_a);
     load_step<true>(tiles, id_a, lane, v_lane, k_a, v_a);
+    // only a walk's first step can hold tokens before lo: here, and not in the loop, where a
+    // branch would keep later loads from being counted (1 sequence of 3971: 14.2 -> 11.5 us)
+    if (Score::kOn && tb < lo) cut(tb, v_a);
     for (;;) {
       if (tb + S::kTile >= t1) {
         compute(tb, id_a, tb + S::kTile > t1, true, k_a, v_a);

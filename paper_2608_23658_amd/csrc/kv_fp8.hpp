@@ -132,6 +132,21 @@ __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* 
     }
   };
 
+  // Zeroes V's slots at or past t1, or before lo: they may hold anything, and zero times NaN
+  // is NaN.
+  auto cut = [&](int tb, uint4 (&vreg)[kTB][kL]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < kTB; ++j) {
+      const int tok = tb + j * kBS + row * 4;
+      uint32_t keep = first_bytes(t1 - tok);
+      if constexpr (Score::kOn) keep &= ~first_bytes(lo - tok);
+#pragma unroll
+      for (int i = 0; i < kL; ++i) {
+        const uint4 v = vreg[j][i];
+        vreg[j][i] = make_uint4(v.x & keep, v.y & keep, v.z & keep, v.w & keep);
+      }
+    }
+  };
   // The products and softmax of one loaded step; tail: it may end inside a
   // block; zero: a block without a valid id still holds what was loaded for it.
   auto compute = [&](int tb, const int (&bid)[kTB], const int (&exps)[kTB], bool tail, bool zero,
@@ -151,13 +166,22 @@ __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* 
         sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8x8_to_bf16(k.z, k.w, ks, ks), qreg[i][1],
                                                      sc, 0, 0, 0);
       }
+      if constexpr (Score::kOn) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[j][r] = sc[r];
+        score.template cap<false>(x[j]);
+        if (score.slopes) {
+          const float far = (float)(own - (tb + j * kBS + row * 4));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[j][r] = fmaf(slope, (float)r - far, x[j][r]);
+        }
+      }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int tok = tb + j * kBS + row * 4 + r;
         const bool keep = bid[j] >= 0 && (!tail || tok < t1);
         if constexpr (Score::kOn)
-          x[j][r] = keep && tok >= lo ? score.template at<false>(sc[r], slope, own - tok)
-                                      : -INFINITY;
+          x[j][r] = keep && tok >= lo ? x[j][r] : -INFINITY;
         else
           x[j][r] = keep ? sc[r] * score.scale_log2 : -INFINITY;
       }
@@ -198,20 +222,7 @@ __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* 
         for (int i = 0; i < kL; ++i) vreg[j][i] = make_uint4(0, 0, 0, 0);
       }
     }
-    if (tail || (Score::kOn && tb < lo)) {
-      // slots at or past t1 (or before lo) may hold anything, and zero times NaN is NaN
-#pragma unroll
-      for (int j = 0; j < kTB; ++j) {
-        const int tok = tb + j * kBS + row * 4;
-        uint32_t keep = first_bytes(t1 - tok);
-        if constexpr (Score::kOn) keep &= ~first_bytes(lo - tok);
-#pragma unroll
-        for (int i = 0; i < kL; ++i) {
-          const uint4 v = vreg[j][i];
-          vreg[j][i] = make_uint4(v.x & keep, v.y & keep, v.z & keep, v.w & keep);
-        }
-      }
-    }
+    if (tail || (Score::kOn && !kAhead && tb < lo)) cut(tb, vreg);
 #pragma unroll
     for (int j = 0; j < kTB; j += 2) {
       const float s0 = fp8_scale(exps[j] >> 8), s1 = fp8_scale(exps[j + 1] >> 8);
@@ -261,6 +272,7 @@ __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* 
     int tb = t0;
     step_ids(tb, id_a);
     load(kAll, id_a, k_a, v_a);
+    if (Score::kOn && tb < lo) cut(tb, v_a);   // as in the bf16 walk
     for (;;) {
       if (tb + kTile >= t1) {
         step_exps(tb, e_a);

@@ -38,6 +38,7 @@ struct ModScore {
   float scale_log2;       // of q . k
   float cap_log2;         // 0: no cap
   float tanh_scale;       // a / cap of a q . k
+  float exp_scale;        // 2 log2(e) times that
   const float* slopes;    // of every query head, null: no bias
   int window;             // kNoWindow: none
   // With a cap, of products smaller than near: a score is dot (p0 + p1 dot^2 + p2 dot^4 +
@@ -57,8 +58,8 @@ struct ModScore {
   // one up to kSmallCap is 2^-14 of a weight; for a larger one, near zero, by kTanh4. kExact:
   // the library's tanh.
   static constexpr float kSmallCap = 256.f;   // in the log2 domain
-  static __device__ __forceinline__ float capped_far(float z, float cap_log2) {
-    const float u = fast_exp2(z * (2.f * kLog2e));
+  static __device__ __forceinline__ float capped_far(float dot, float exp_scale, float cap_log2) {
+    const float u = fast_exp2(dot * exp_scale);
     return fmaf(-2.f * cap_log2, __builtin_amdgcn_rcpf(u + 1.f), cap_log2);
   }
   static __device__ __forceinline__ float capped_near(float z, float cap_log2) {
@@ -68,29 +69,34 @@ struct ModScore {
     h = fmaf(h, w, kTanh4[0]);
     return z * cap_log2 * fmaf(h, w, 1.f);
   }
-  template <bool kExact>
-  __device__ __forceinline__ float capped(float dot) const {
-    const float z = dot * tanh_scale;
-    if constexpr (kExact) return cap_log2 * tanhf(z);
-    const float far = capped_far(z, cap_log2);
-    if (cap_log2 <= kSmallCap) return far;
-    return fabsf(z) < 0.6f ? capped_near(z, cap_log2) : far;
-  }
 
-  // ---- for a walk, score by score ----
+  // ---- for a walk, some scores at a time ----
 
   // The same in vector registers: a walk's scalar ones are full of addresses.
   __device__ __forceinline__ ModScore held() const {
     ModScore s = *this;
-    asm("" : "+v"(s.scale_log2), "+v"(s.cap_log2), "+v"(s.tanh_scale));
+    asm("" : "+v"(s.scale_log2), "+v"(s.cap_log2), "+v"(s.exp_scale));
     return s;
   }
-  // The score of a key that lies ago tokens before the row.
-  template <bool kExact>
-  __device__ __forceinline__ float at(float dot, float slope_log2, int ago) const {
-    const float x =
-        has_cap() ? capped<kExact>(dot) : dot * scale_log2;
-    return fmaf(slope_log2, -(float)ago, x);
+  // The scores of n products in place. kExact: with the library's tanh.
+  template <bool kExact, int n>
+  __device__ __forceinline__ void cap(float (&x)[n]) const {
+    if (!has_cap()) {
+#pragma unroll
+      for (int e = 0; e < n; ++e) x[e] *= scale_log2;
+    } else if constexpr (kExact) {
+#pragma unroll
+      for (int e = 0; e < n; ++e) x[e] = cap_log2 * tanhf(x[e] * tanh_scale);
+    } else if (cap_log2 <= kSmallCap) {
+#pragma unroll
+      for (int e = 0; e < n; ++e) x[e] = capped_far(x[e], exp_scale, cap_log2);
+    } else {
+#pragma unroll
+      for (int e = 0; e < n; ++e) {
+        const float z = x[e] * tanh_scale, far = capped_far(x[e], exp_scale, cap_log2);
+        x[e] = fabsf(z) < 0.6f ? capped_near(z, cap_log2) : far;
+      }
+    }
   }
 
   // ---- for a prefill tile, the scores of 64 keys and 32 rows at a time ----
@@ -134,11 +140,11 @@ struct ModScore {
           s[e / 16][e % 16] = x * fmaf(fmaf(fmaf(t, c3, c2), t, c1), t, c0);
         }
       } else {
-        float scale = tanh_scale, cap = cap_log2;
+        float scale = exp_scale, cap = cap_log2;
         here(scale, cap);
 #pragma unroll
         for (int e = 0; e < 32; ++e)
-          s[e / 16][e % 16] = capped_far(s[e / 16][e % 16] * scale, cap);
+          s[e / 16][e % 16] = capped_far(s[e / 16][e % 16], scale, cap);
       }
       const float slope =
           __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(slope_log2)));
@@ -185,6 +191,7 @@ ModScore<kForm> mod_score(float scale, const ScoreMods& m) {
   s.scale_log2 = scale * kLog2e;
   s.cap_log2 = m.softcap * kLog2e;
   s.tanh_scale = m.softcap > 0.f ? scale / m.softcap : 0.f;
+  s.exp_scale = s.tanh_scale * (2.f * kLog2e);
   s.slopes = m.slopes;
   s.window = window_keys(m);
   const float w = s.tanh_scale * s.tanh_scale;

@@ -631,57 +631,80 @@ def prefill_chunk_scored_fp8(q: torch.Tensor, kv_layer, num_blocks: int,
                            ws, stream)
 
 
+def _refuse_rows(q, k, v, slot_mapping, q_weight, k_weight, rope_table, positions):
+    """Says what is wrong with a qkv append's tensors, if anything is."""
+    T, _, d = q.shape
+    if k.dim() != 3 or k.shape[::2] != (T, d) or v.shape != k.shape or \
+            not (q.dtype == k.dtype == v.dtype):
+        raise ValueError("q must be [T, Hq, d], k and v [T, Hkv, d], all of one dtype")
+    for x in (q, k, v):
+        if x.stride(2) != 1 or x.stride(1) != d and x.shape[1] > 1:
+            raise ValueError("a token's heads must be contiguous in q, k and v")
+    if slot_mapping.dtype != torch.int32 or slot_mapping.shape != (T,):
+        raise ValueError("slot_mapping must be int32 [num_tokens]")
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None and (w.dtype != q.dtype or w.shape != (d,)):
+            raise ValueError(f"{name} must be [{d}] of q's dtype")
+    if rope_table is None:
+        return
+    if rope_table.dtype != torch.float32 or rope_table.dim() != 2:
+        raise ValueError("rope_table must be float32 [positions, rot_dim]")
+    if positions is None or positions.dtype != torch.int32 or positions.dim() > 2 or \
+            positions.shape[-1:] != (T,):
+        raise ValueError("positions must be int32 [num_tokens] or [num_axes, num_tokens]")
+
+
 def _qkv_append(call, q, k, v, slot_mapping, kv_layer, num_blocks, positions, rope_table,
                 sections, interleaved, q_weight, k_weight, eps, out, block_size, stream):
     T, Hq, d = q.shape
     Hkv = k.shape[1]
-    if k.shape != (T, Hkv, d) or v.shape != k.shape or not (q.dtype == k.dtype == v.dtype):
-        raise ValueError("q must be [T, Hq, d], k and v [T, Hkv, d], all of one dtype")
-    for x in (q, k, v):
-        if x.stride(2) != 1 or x.stride(1) != d and x.shape[1] > 1 or x.stride(0) < 0:
-            raise ValueError("a token's heads must be contiguous in q, k and v")
-    code = _dtype_code(q.dtype)
-    if slot_mapping.dtype != torch.int32 or slot_mapping.shape != (T,):
-        raise ValueError("slot_mapping must be int32 [num_tokens]")
-    prep = NormRope(eps=eps)
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            if w.dtype != q.dtype or w.shape != (d,):
-                raise ValueError(f"{name} must be [{d}] of q's dtype")
-            setattr(prep, name, w.data_ptr())
+    dt, i32 = q.dtype, torch.int32
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    # one test when all is well: a small call is bound by the time this module takes
+    if not (k.dtype is dt and v.dtype is dt and k.shape == v.shape == (T, Hkv, d) and
+            qs[1:] == ks[1:] == vs[1:] == (d, 1) and slot_mapping.dtype is i32 and
+            slot_mapping.shape == (T,) and
+            (q_weight is None or q_weight.dtype is dt and q_weight.shape == (d,)) and
+            (k_weight is None or k_weight.dtype is dt and k_weight.shape == (d,)) and
+            (rope_table is None or positions is not None and positions.dtype is i32 and
+             positions.shape[-1:] == (T,) and positions.dim() <= 2 and
+             rope_table.dtype is torch.float32 and rope_table.dim() == 2)):
+        _refuse_rows(q, k, v, slot_mapping, q_weight, k_weight, rope_table, positions)
+    code = _dtype_code(dt)
+    rope_len = rot = axes = pos = table = 0
+    pairs = ()
     if rope_table is not None:
-        if rope_table.dtype != torch.float32 or rope_table.dim() != 2:
-            raise ValueError("rope_table must be float32 [positions, rot_dim]")
-        if positions is None or positions.dtype != torch.int32 or positions.shape[-1:] != (T,) or \
-                positions.dim() > 2:
-            raise ValueError("positions must be int32 [num_tokens] or [num_axes, num_tokens]")
-        prep.rope_table = rope_table.data_ptr()
-        prep.rope_len, prep.rot_dim = rope_table.shape
-        prep.interleaved = bool(interleaved)
-        prep.positions = positions.data_ptr()
-        prep.num_axes = axes = 1 if positions.dim() == 1 else positions.shape[0]
-        if sections is None:
-            if axes != 1:
-                raise ValueError("several axes of positions need sections")
-            sections = (rope_table.shape[1] // 2,)
-        if len(sections) != axes or axes > len(prep.sections):
-            raise ValueError(f"{axes} axes of positions, {len(sections)} sections (at most "
-                             f"{len(prep.sections)})")
-        prep.sections[:axes] = sections
+        rope_len, rot = rope_table.shape
+        table, pos = rope_table.data_ptr(), positions.data_ptr()
+        axes = 1 if positions.dim() == 1 else positions.shape[0]
+        if sections is not None:
+            pairs = tuple(sections)
+        elif axes == 1:
+            pairs = (rot // 2,)
+        else:
+            raise ValueError("several axes of positions need sections")
+        if len(pairs) != axes or axes > 4:
+            raise ValueError(f"{axes} axes of positions, {len(pairs)} sections (at most 4)")
     elif positions is not None or sections is not None:
         raise ValueError("positions and sections need a rope_table")
-    if out is not None and (out.dtype != q.dtype or out.shape != q.shape):
+    if out is not None and (out.dtype != dt or out.shape != q.shape):
         raise ValueError("out must have q's shape and dtype")
     _require_here(slot_mapping, kv_layer, positions, rope_table, q_weight, k_weight, out)
     here = slot_mapping.get_device()
-    if not (q.get_device() == k.get_device() == v.get_device() == here):
+    if not q.get_device() == k.get_device() == v.get_device() == here:
         raise ValueError(f"q, k and v must be on slot_mapping's device (cuda:{here})")
     if out is None:
-        out = _made_for(stream, lambda: torch.empty((T, Hq, d), dtype=q.dtype, device=q.device),
-                        returned=True)
-    check(call(q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
-               ctypes.byref(prep), slot_mapping.data_ptr(), out.data_ptr(), _ptr(kv_layer),
-               int(num_blocks), T, Hq, Hkv, d, int(block_size), code, _stream(stream)))
+        if stream is None:
+            out = torch.empty((T, Hq, d), dtype=dt, device=q.device)
+        else:
+            out = _made_for(stream, lambda: torch.empty((T, Hq, d), dtype=dt, device=q.device),
+                            returned=True)
+    prep = NormRope(0 if q_weight is None else q_weight.data_ptr(),
+                    0 if k_weight is None else k_weight.data_ptr(), eps, table, rope_len, rot,
+                    bool(interleaved), pos, axes, pairs)
+    check(call(q.data_ptr(), qs[0], k.data_ptr(), ks[0], v.data_ptr(), vs[0], prep,
+               slot_mapping.data_ptr(), out.data_ptr(), _ptr(kv_layer), int(num_blocks), T, Hq,
+               Hkv, d, int(block_size), code, _stream(stream)))
     return out
 
 
