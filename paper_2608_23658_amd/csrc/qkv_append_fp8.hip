@@ -8,81 +8,22 @@
 
 namespace kvattn {
 
-// Norm and rotation of K rows as append_fp8 holds them: a row's 16-byte pieces in 8 or 16
-// neighbouring lanes (D elements of fp32: 32 pieces, two in each of 16 lanes).
-// kRotDim 0: no rotation.
+// Norm and rotation of K rows as append_fp8 holds them, along the lanes.
 template <int ESZ, int D, int kRotDim, bool kEven>
 struct KeyPrep {
   static constexpr bool kOn = true;
-  static constexpr int kVec = 16 / ESZ, kCh = D / kVec;
-  static constexpr int kPer = kCh > 16 ? kCh / 16 : 1;   // pieces of a row in a lane
-  static constexpr int kOff = kRotDim / 2 / kVec;        // pieces between the two of a pair
+  using R = LaneRows<ESZ, D, kRotDim, kEven>;
   const QkvArgs& a;
 
-  // The kPer pieces x of token t, the first of them the row's piece-th.
+  // The lane's pieces x of token t, the first of them the row's piece-th.
   __device__ __forceinline__ void apply(float* x, int t, int piece) const {
+    float c[R::kPairs], s[R::kPairs], w[R::kElems];
+    R::turns(a, t, piece, c, s);
     if (a.k_weight) {
-      float sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < kPer * kVec; ++e) sum = fmaf(x[e], x[e], sum);
-      sum += dpp_mov<kDppQuadSwap1>(sum);
-      sum += dpp_mov<kDppQuadSwap2>(sum);
-      sum += dpp_mov<kDppRowHalfMirror>(sum);
-      if constexpr (kCh > 8) sum += dpp_mov<kDppRowMirror>(sum);
-      const float by = rsqrtf(fmaf(sum, 1.f / D, a.eps));
-#pragma unroll
-      for (int p = 0; p < kPer; ++p) {
-        float w[kVec];
-        QkvRows<ESZ, D, 0, false>::widen(
-            reinterpret_cast<const uint4*>(a.k_weight)[piece + 16 * p], w);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) x[p * kVec + e] = x[p * kVec + e] * by * w[e];
-      }
+      R::weights(a.k_weight, piece, w);
+      R::norm(x, w, a.eps);
     }
-    if constexpr (kRotDim > 0) {
-#pragma unroll
-      for (int p = 0; p < kPer; ++p) {
-        if constexpr (kEven) {
-          if ((piece + 16 * p) * kVec < kRotDim) {
-#pragma unroll
-            for (int m = 0; m < kVec / 2; ++m) {
-              const float2 cs = turn_of((piece + 16 * p) * (kVec / 2) + m, t);
-              turn(x[p * kVec + 2 * m], x[p * kVec + 2 * m + 1], cs);
-            }
-          }
-        } else if constexpr (kOff >= 16) {   // both of a pair in the lane
-          if (p < kPer / 2) {
-#pragma unroll
-            for (int e = 0; e < kVec; ++e)
-              turn(x[p * kVec + e], x[(p + kPer / 2) * kVec + e],
-                   turn_of((piece + 16 * p) * kVec + e, t));
-          }
-        } else if (p == 0) {                 // the pair's other dim kOff lanes away
-          const bool in = piece < 2 * kOff, second = piece & kOff;
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) {
-            const float other = __shfl_xor(x[e], kOff, kWave);
-            if (in) {
-              const float2 cs = turn_of(piece % kOff * kVec + e, t);
-              x[e] = fmaf(x[e], cs.x, second ? other * cs.y : -other * cs.y);
-            }
-          }
-        }
-      }
-    }
-  }
-
-  static __device__ __forceinline__ void turn(float& u, float& v, float2 cs) {
-    QkvRows<ESZ, D, 0, false>::turn(u, v, cs.x, cs.y);
-  }
-
-  // Cosine and sine of pair p for token t; NaN for a position outside the table.
-  __device__ __forceinline__ float2 turn_of(int p, int t) const {
-    const int axis = (p >= a.axis_end[0]) + (p >= a.axis_end[1]) + (p >= a.axis_end[2]);
-    const int pos = a.positions[(size_t)axis * a.num_tokens + t];
-    const bool in = (unsigned)pos < (unsigned)a.table_len;
-    const float* at = a.table + (size_t)(in ? pos : 0) * kRotDim + p;
-    return in ? make_float2(at[0], at[kRotDim / 2]) : make_float2(NAN, NAN);
+    R::rotate(x, piece, c, s);
   }
 };
 
@@ -97,8 +38,7 @@ __global__ __launch_bounds__(kQkvWaves * kWave) void qkv_append_fp8_kernel(QkvAr
                              a.num_tokens, a.num_kv_heads, a.num_blocks * kBS,
                              KeyPrep<ESZ, D, kRotDim, kEven>{a});
   else
-    qkv_rows<ESZ, D, kRotDim * ESZ / 64, kEven, false>(a, blockIdx.x - append_wgs, groups,
-                                                       per_wave);
+    q_rows<ESZ, D, kRotDim, kEven>(a, blockIdx.x - append_wgs, groups, per_wave);
 }
 
 template <int ESZ, int D, int kRotDim, bool kEven>

@@ -1,12 +1,5 @@
-// Norm and rotation of a run of q or k rows, held by one wavefront in the order in which
-// the cache's K tile has them.
-//
-// A wavefront has one head's rows of 16 consecutive tokens: lane l has token l % 16 and,
-// of its row's 16-byte chunks, chunk 4 i + l / 16 in register i. So a register's 64 lanes
-// are 1 KiB of a K tile as it lies in the cache; a row's sum is a lane's own and one
-// exchange between the four lanes of a row; and the two dims of a pair, half the rotated
-// dims apart, are a whole number of registers apart in the same lane (32 rotated dims of
-// bf16 excepted: there they are two lanes of a row).
+// Norm and rotation of q and k rows in registers, in the two orders that the kernels hold
+// them in.
 #pragma once
 
 #include <type_traits>
@@ -21,81 +14,10 @@ constexpr int kRunTokens = 16;   // tokens of a run, slots of a block
 constexpr int kQkvWaves = 4;
 }  // namespace
 
-// kRot: registers of rotated chunks (0: no rotation). kEven: pairs are adjacent dims.
-template <int ESZ, int D, int kRot, bool kEven>
-struct QkvRows {
-  static constexpr int kVec = 16 / ESZ;            // elements per chunk
-  static constexpr int kN = D / kVec / 4;          // chunks per lane
-  static constexpr int kElems = kN * kVec;
-  static constexpr int kRotDim = kRot * 4 * kVec;
-  static constexpr bool kSwap = kRot == 1 && !kEven;   // a pair is in two lanes
-  static constexpr int kPairs = kSwap ? kVec : kRot * kVec / 2;   // cosines per lane
-  static constexpr int kRun = kEven && kRot ? kVec / 2 : kVec;    // of them in a row of the table
-  static_assert(kRot <= kN && (kRot % 2 == 0 || kRot == 1), "whole registers");
-
-  float cs[kPairs ? kPairs : 1], sn[kPairs ? kPairs : 1];
-  float w[kElems];   // the norm's weight
-
-  static __device__ __forceinline__ int row() { return threadIdx.x % kWave / 16; }
-
-  // First pair of the lane's i-th run of kRun pairs.
-  static __device__ __forceinline__ int first_pair(int i) {
-    return kSwap ? row() % 2 * kVec : (4 * i + row()) * kRun;
-  }
-
-  // The cosines and sines of token t's positions. A position outside the table gives NaN.
-  __device__ __forceinline__ void load_turns(const QkvArgs& a, int t) {
-    if constexpr (kRot > 0) {
-      constexpr int kHalf = kRotDim / 2;
-      const bool one = a.axis_end[0] >= kHalf;
-#pragma unroll
-      for (int i = 0; i < kPairs / kRun; ++i) {
-        const int p0 = first_pair(i);
-        float* c = cs + i * kRun;
-        float* s = sn + i * kRun;
-        if (one) {
-          const int pos = a.positions[t];
-          const bool in = (unsigned)pos < (unsigned)a.table_len;
-          const float* at = a.table + (size_t)(in ? pos : 0) * kRotDim + p0;
-          load_run(at, c);
-          load_run(at + kHalf, s);
-          if (!in) {
-#pragma unroll
-            for (int e = 0; e < kRun; ++e) c[e] = s[e] = NAN;
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < kRun; ++e) {
-            const int p = p0 + e;
-            const int axis = (p >= a.axis_end[0]) + (p >= a.axis_end[1]) + (p >= a.axis_end[2]);
-            const int pos = a.positions[(size_t)axis * a.num_tokens + t];
-            const bool in = (unsigned)pos < (unsigned)a.table_len;
-            const float* at = a.table + (size_t)(in ? pos : 0) * kRotDim + p;
-            c[e] = in ? at[0] : NAN;
-            s[e] = in ? at[kHalf] : NAN;
-          }
-        }
-      }
-    }
-  }
-
-  static __device__ __forceinline__ void load_run(const float* at, float* to) {
-    if constexpr (kRun % 4 == 0) {
-#pragma unroll
-      for (int e = 0; e < kRun; e += 4) {
-        const float4 v = *reinterpret_cast<const float4*>(at + e);
-        to[e] = v.x;
-        to[e + 1] = v.y;
-        to[e + 2] = v.z;
-        to[e + 3] = v.w;
-      }
-    } else {
-      const float2 v = *reinterpret_cast<const float2*>(at);
-      to[0] = v.x;
-      to[1] = v.y;
-    }
-  }
-
+// ESZ: bytes of an element. Values are fp32 between a row's load and its store.
+template <int ESZ>
+struct QkvPieces {
+  static constexpr int kVec = 16 / ESZ;   // elements of a 16-byte piece
   static __device__ __forceinline__ void widen(uint4 v, float* x) {
     const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -117,12 +39,186 @@ struct QkvRows {
       return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
                         __float_as_uint(x[3]));
   }
+};
+
+// (a, b) turned by an angle of cosine c and sine s.
+__device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
+  const float a1 = fmaf(a, c, -(b * s));
+  b = fmaf(b, c, a * s);
+  a = a1;
+}
+
+// The cosines and sines of pairs p .. p + n of token t, n 2 or a multiple of 4. A position
+// outside the table gives NaN.
+template <int kRotDim, int n>
+__device__ __forceinline__ void load_turns(const QkvArgs& a, int t, int p, float* c, float* s) {
+  constexpr int kHalf = kRotDim / 2;
+  if (a.axis_end[0] >= kHalf) {   // one axis
+    const int pos = a.positions[t];
+    const bool in = (unsigned)pos < (unsigned)a.table_len;
+    const float* at = a.table + (size_t)(in ? pos : 0) * kRotDim + p;
+    if constexpr (n % 4 == 0) {
+#pragma unroll
+      for (int e = 0; e < n; e += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(at + e);
+        const float4 y = *reinterpret_cast<const float4*>(at + kHalf + e);
+        c[e] = x.x; c[e + 1] = x.y; c[e + 2] = x.z; c[e + 3] = x.w;
+        s[e] = y.x; s[e + 1] = y.y; s[e + 2] = y.z; s[e + 3] = y.w;
+      }
+    } else {
+      const float2 x = *reinterpret_cast<const float2*>(at);
+      const float2 y = *reinterpret_cast<const float2*>(at + kHalf);
+      c[0] = x.x; c[1] = x.y;
+      s[0] = y.x; s[1] = y.y;
+    }
+    if (!in) {
+#pragma unroll
+      for (int e = 0; e < n; ++e) c[e] = s[e] = NAN;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < n; ++e) {
+      const int axis = (p + e >= a.axis_end[0]) + (p + e >= a.axis_end[1]) +
+                       (p + e >= a.axis_end[2]);
+      const int pos = a.positions[(size_t)axis * a.num_tokens + t];
+      const bool in = (unsigned)pos < (unsigned)a.table_len;
+      const float* at = a.table + (size_t)(in ? pos : 0) * kRotDim + p + e;
+      c[e] = in ? at[0] : NAN;
+      s[e] = in ? at[kHalf] : NAN;
+    }
+  }
+}
+
+// ---- rows along the lanes ----
+// A row's 16-byte pieces lie in 8 or 16 neighbouring lanes (512 bytes: two in each of 16),
+// so that rows are read and written as they lie. kRotDim 0: no rotation.
+template <int ESZ, int D, int kRotDim, bool kEven>
+struct LaneRows {
+  using P = QkvPieces<ESZ>;
+  static constexpr int kVec = P::kVec, kCh = D / kVec;
+  static constexpr int kPer = kCh > 16 ? kCh / 16 : 1;   // pieces of a row in a lane
+  static constexpr int kLanes = kCh / kPer;              // lanes of a row
+  static constexpr int kElems = kPer * kVec;
+  static constexpr int kOff = kRotDim / 2 / kVec;        // pieces between the two of a pair
+  static constexpr bool kInLane = kEven || kOff >= 16;   // both of a pair in a lane
+  static constexpr int kPairs = kRotDim == 0 ? 1 : kInLane ? kElems / 2 : kVec;
+
+  // The cosines and sines that a lane with pieces piece, piece + 16 needs of token t.
+  static __device__ __forceinline__ void turns(const QkvArgs& a, int t, int piece, float (&c)[kPairs],
+                                               float (&s)[kPairs]) {
+    if constexpr (kRotDim > 0) {
+#pragma unroll
+      for (int p = 0; p < kPer; ++p) {
+        if constexpr (kEven) {
+          if ((piece + 16 * p) * kVec < kRotDim)
+            load_turns<kRotDim, kVec / 2>(a, t, (piece + 16 * p) * (kVec / 2), c + p * (kVec / 2),
+                                          s + p * (kVec / 2));
+        } else if constexpr (kInLane) {
+          if (p < kPer / 2)
+            load_turns<kRotDim, kVec>(a, t, (piece + 16 * p) * kVec, c + p * kVec, s + p * kVec);
+        } else if (p == 0 && piece < 2 * kOff) {
+          load_turns<kRotDim, kVec>(a, t, piece % kOff * kVec, c, s);
+        }
+      }
+    }
+  }
+  static __device__ __forceinline__ void weights(const uint8_t* weight, int piece,
+                                                 float (&w)[kElems]) {
+#pragma unroll
+    for (int p = 0; p < kPer; ++p)
+      P::widen(reinterpret_cast<const uint4*>(weight)[piece + 16 * p], w + p * kVec);
+  }
+  // x * rsqrt(mean(x^2) + eps) * w
+  static __device__ __forceinline__ void norm(float* x, const float (&w)[kElems], float eps) {
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < kElems; ++e) sum = fmaf(x[e], x[e], sum);
+    sum += dpp_mov<kDppQuadSwap1>(sum);
+    sum += dpp_mov<kDppQuadSwap2>(sum);
+    sum += dpp_mov<kDppRowHalfMirror>(sum);
+    if constexpr (kLanes > 8) sum += dpp_mov<kDppRowMirror>(sum);
+    const float by = rsqrtf(fmaf(sum, 1.f / D, eps));
+#pragma unroll
+    for (int e = 0; e < kElems; ++e) x[e] = x[e] * by * w[e];
+  }
+  // The same dim of the piece kOff lanes away in the row (xor).
+  static __device__ __forceinline__ float across(float x) {
+    if constexpr (kOff == 8) return dpp_mov<0x128>(x);          // rotate 16 lanes by 8
+    if constexpr (kOff == 2) return dpp_mov<kDppQuadSwap2>(x);
+    if constexpr (kOff == 4) return dpp_mov<kDppRowHalfMirror>(dpp_mov<0x1b>(x));   // 7 - (3 - i)
+    return x;
+  }
+  static __device__ __forceinline__ void rotate(float* x, int piece, const float (&c)[kPairs],
+                                                const float (&s)[kPairs]) {
+    if constexpr (kRotDim == 0) return;
+    if constexpr (kEven) {
+#pragma unroll
+      for (int p = 0; p < kPer; ++p)
+        if ((piece + 16 * p) * kVec < kRotDim) {
+#pragma unroll
+          for (int m = 0; m < kVec / 2; ++m)
+            turn(x[p * kVec + 2 * m], x[p * kVec + 2 * m + 1], c[p * (kVec / 2) + m],
+                 s[p * (kVec / 2) + m]);
+        }
+    } else if constexpr (kInLane) {
+#pragma unroll
+      for (int e = 0; e < kElems / 2; ++e) turn(x[e], x[e + kElems / 2], c[e], s[e]);
+    } else {
+      const bool in = piece < 2 * kOff, second = piece & kOff;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const float other = across(x[e]);
+        const float y = fmaf(x[e], c[e], second ? other * s[e] : -other * s[e]);
+        x[e] = in ? y : x[e];
+      }
+    }
+  }
+};
+
+// ---- rows across the lanes, in the order of the cache's K tile ----
+// A wavefront has one head's rows of 16 tokens: lane l has token l % 16 and, of its row's
+// 16-byte chunks, chunk 4 i + l / 16 in register i. So a register's 64 lanes are 1 KiB of
+// a K tile as it lies in the cache; a row's sum is a lane's own and one exchange between the
+// four lanes of a row; and the two dims of a pair, half the rotated dims apart, are a whole
+// number of registers apart in the same lane (32 rotated dims of bf16 excepted: there they
+// are two lanes of a row).
+// kRot: registers of rotated chunks (0: no rotation). kEven: pairs are adjacent dims.
+template <int ESZ, int D, int kRot, bool kEven>
+struct TileRows {
+  using P = QkvPieces<ESZ>;
+  static constexpr int kVec = 16 / ESZ;            // elements per chunk
+  static constexpr int kN = D / kVec / 4;          // chunks per lane
+  static constexpr int kElems = kN * kVec;
+  static constexpr int kRotDim = kRot * 4 * kVec;
+  static constexpr bool kSwap = kRot == 1 && !kEven;   // a pair is in two lanes
+  static constexpr int kPairs = kSwap ? kVec : kRot * kVec / 2;   // cosines per lane
+  static constexpr int kRun = kEven && kRot ? kVec / 2 : kVec;    // of them in a row of the table
+  static_assert(kRot <= kN && (kRot % 2 == 0 || kRot == 1), "whole registers");
+
+  float cs[kPairs ? kPairs : 1], sn[kPairs ? kPairs : 1];
+  float w[kElems];   // the norm's weight
+
+  static __device__ __forceinline__ int row() { return threadIdx.x % kWave / 16; }
+
+  // First pair of the lane's i-th run of kRun pairs.
+  static __device__ __forceinline__ int first_pair(int i) {
+    return kSwap ? row() % 2 * kVec : (4 * i + row()) * kRun;
+  }
+
+  // The cosines and sines of token t's positions.
+  __device__ __forceinline__ void load(const QkvArgs& a, int t) {
+    if constexpr (kRot > 0) {
+#pragma unroll
+      for (int i = 0; i < kPairs / kRun; ++i)
+        load_turns<kRotDim, kRun>(a, t, first_pair(i), cs + i * kRun, sn + i * kRun);
+    }
+  }
 
   __device__ __forceinline__ void load_weight(const uint8_t* weight) {
     if (!weight) return;
 #pragma unroll
     for (int i = 0; i < kN; ++i)
-      widen(reinterpret_cast<const uint4*>(weight)[4 * i + row()], w + i * kVec);
+      P::widen(reinterpret_cast<const uint4*>(weight)[4 * i + row()], w + i * kVec);
   }
 
   // x * rsqrt(mean(x^2) + eps) * w, in fp32
@@ -151,94 +247,56 @@ struct QkvRows {
       for (int p = 0; p < kPairs; ++p) turn(x[p], x[p + kPairs], cs[p], sn[p]);
     }
   }
-  static __device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
-    const float a1 = fmaf(a, c, -(b * s));
-    b = fmaf(b, c, a * s);
-    a = a1;
-  }
 };
 
-// The work of workgroup wg, of (runs x groups of heads): per_wave heads a wavefront, of q
-// and, with kCache, k and v too.
-template <int ESZ, int D, int kRot, bool kEven, bool kCache>
-__device__ __forceinline__ void qkv_rows(const QkvArgs& a, int wg, int groups, int per_wave) {
-  using R = QkvRows<ESZ, D, kRot, kEven>;
+// The q rows of workgroup wg, of (runs x groups of heads): per_wave heads a wavefront, the
+// next one's rows on their way while one's are computed.
+template <int ESZ, int D, int kRotDim, bool kEven>
+__device__ __forceinline__ void q_rows(const QkvArgs& a, int wg, int groups, int per_wave) {
+  using R = LaneRows<ESZ, D, kRotDim, kEven>;
+  constexpr int kRows = kRunTokens * R::kLanes / kWave;   // rows of a lane
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int row = lane / 16;
-  const int hq = a.num_q_heads, hkv = a.num_kv_heads;
-  const int heads = kCache ? hq + 2 * hkv : hq;
+  const int hq = a.num_q_heads;
   const int h0 = (wg % groups * kQkvWaves + wave) * per_wave;
-  const int h1 = min(heads, h0 + per_wave);
+  const int h1 = min(hq, h0 + per_wave);
   if (h0 >= h1) return;
-  const int t = wg / groups * kRunTokens + lane % 16;
-  const bool real = t < a.num_tokens;
-  const int tc = min(t, a.num_tokens - 1);
-
-  R rows;
-  if (h0 < hq + hkv) rows.load_turns(a, tc);
-  uint8_t* block = nullptr;    // of the token's slot; null: it has none
-  int slot = 0;
-  constexpr size_t kTile = (size_t)kRunTokens * D * ESZ;
-  if (kCache && h1 > hq && real) {
-    slot = a.slot_mapping[t];
-    if ((unsigned)slot < (unsigned)(a.num_blocks * kRunTokens)) {
-      block = a.kv + (size_t)(slot / kRunTokens) * (2 * (size_t)hkv * kTile);
-      slot %= kRunTokens;
-    }
-  }
-
-  const uint8_t* weight = nullptr;
-  for (int h = h0; h < h1; ++h) {
-    const bool is_q = !kCache || h < hq, is_v = kCache && h >= hq + hkv;
-    const int g = is_q ? h : is_v ? h - hq - hkv : h - hq;
-    const uint8_t* src = (is_q ? a.q + (size_t)tc * a.q_stride
-                               : is_v ? a.v + (size_t)tc * a.v_stride
-                                      : a.k + (size_t)tc * a.k_stride) +
-                         (size_t)g * (D * ESZ);
-    uint4 raw[R::kN];
+  const int t0 = wg / groups * kRunTokens + lane / R::kLanes, piece = lane % R::kLanes;
+  auto token = [&](int r) { return t0 + r * (kWave / R::kLanes); };
+  auto load = [&](int h, uint4 (&x)[kRows * R::kPer]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < R::kN; ++i) raw[i] = reinterpret_cast<const uint4*>(src)[4 * i + row];
-    if (!is_v) {
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+      for (int p = 0; p < R::kPer; ++p)
+        x[r * R::kPer + p] =
+            load_nt(reinterpret_cast<const uint4*>(
+                        a.q + (size_t)min(token(r), a.num_tokens - 1) * a.q_stride +
+                        (size_t)h * (D * ESZ)) + piece + 16 * p);
+  };
+  uint4 next[kRows * R::kPer];
+  load(h0, next);
+  float w[R::kElems];
+  if (a.q_weight) R::weights(a.q_weight, piece, w);
+  float c[kRows][R::kPairs], s[kRows][R::kPairs];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r)
+    R::turns(a, min(token(r), a.num_tokens - 1), piece, c[r], s[r]);
+  for (int h = h0; h < h1; ++h) {
+    uint4 raw[kRows * R::kPer];
+#pragma unroll
+    for (int i = 0; i < kRows * R::kPer; ++i) raw[i] = next[i];
+    if (h + 1 < h1) load(h + 1, next);
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
       float x[R::kElems];
 #pragma unroll
-      for (int i = 0; i < R::kN; ++i) R::widen(raw[i], x + i * R::kVec);
-      const uint8_t* wanted = is_q ? a.q_weight : a.k_weight;
-      if (wanted) {
-        if (wanted != weight) rows.load_weight(wanted);
-        weight = wanted;
-        rows.norm(x, a.eps);
-      }
-      rows.rotate(x);
+      for (int p = 0; p < R::kPer; ++p) R::P::widen(raw[r * R::kPer + p], x + p * R::kVec);
+      if (a.q_weight) R::norm(x, w, a.eps);
+      R::rotate(x, piece, c[r], s[r]);
+      if (token(r) < a.num_tokens) {
+        uint4* to = reinterpret_cast<uint4*>(a.q_out + ((size_t)token(r) * hq + h) * (D * ESZ));
 #pragma unroll
-      for (int i = 0; i < R::kN; ++i) raw[i] = R::narrow(x + i * R::kVec);
-      if (is_q) {
-        if (real) {
-          uint4* to = reinterpret_cast<uint4*>(a.q_out + ((size_t)t * hq + g) * (D * ESZ));
-#pragma unroll
-          for (int i = 0; i < R::kN; ++i) to[4 * i + row] = raw[i];
-        }
-      } else if (block) {
-        uint4* to = reinterpret_cast<uint4*>(block + g * kTile);
-#pragma unroll
-        for (int i = 0; i < R::kN; ++i) to[(4 * i + row) * kRunTokens + slot] = raw[i];
-      }
-    } else if (block) {
-      uint8_t* to = block + (hkv + g) * kTile;
-#pragma unroll
-      for (int i = 0; i < R::kN; ++i) {
-        const uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-        const int j0 = (4 * i + row) * R::kVec;
-        if constexpr (ESZ == 2) {
-          uint16_t* v = reinterpret_cast<uint16_t*>(to);
-#pragma unroll
-          for (int e = 0; e < R::kVec; ++e)
-            v[(j0 + e) * kRunTokens + slot] = (uint16_t)(u[e / 2] >> (16 * (e % 2)));
-        } else {
-          uint32_t* v = reinterpret_cast<uint32_t*>(to);
-#pragma unroll
-          for (int e = 0; e < R::kVec; ++e) v[(j0 + e) * kRunTokens + slot] = u[e];
-        }
+        for (int p = 0; p < R::kPer; ++p) to[piece + 16 * p] = R::P::narrow(x + p * R::kVec);
       }
     }
   }
@@ -252,7 +310,7 @@ struct QkvSplit {
 inline QkvSplit qkv_split(int tokens, int heads) {
   const long long runs = ((long long)tokens + kRunTokens - 1) / kRunTokens;
   QkvSplit s;
-  s.per_wave = runs * heads > 16384 ? 4 : 1;
+  s.per_wave = runs * heads > 8192 ? 8 : runs * heads > 4096 ? 4 : runs * heads > 2048 ? 2 : 1;
   s.groups = (heads + kQkvWaves * s.per_wave - 1) / (kQkvWaves * s.per_wave);
   s.workgroups = runs * s.groups;
   return s;
