@@ -48,43 +48,59 @@ __device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
   a = a1;
 }
 
-// The cosines and sines of pairs p .. p + n of token t, n 2 or a multiple of 4. A position
-// outside the table gives NaN.
+// The cosines and sines of n = 2 or 4 pairs from p on, at position pos. One outside the table
+// gives NaN. p is a multiple of n, a table's row of 4 floats.
+template <int kRotDim, int n>
+__device__ __forceinline__ void load_turns_at(const QkvArgs& a, int pos, int p, float* c,
+                                              float* s) {
+  const bool in = (unsigned)pos < (unsigned)a.table_len;
+  const float* at = a.table + (size_t)(in ? pos : 0) * kRotDim + p;
+  if constexpr (n == 4) {
+    const float4 x = *reinterpret_cast<const float4*>(at);
+    const float4 y = *reinterpret_cast<const float4*>(at + kRotDim / 2);
+    c[0] = x.x; c[1] = x.y; c[2] = x.z; c[3] = x.w;
+    s[0] = y.x; s[1] = y.y; s[2] = y.z; s[3] = y.w;
+  } else {
+    const float2 x = *reinterpret_cast<const float2*>(at);
+    const float2 y = *reinterpret_cast<const float2*>(at + kRotDim / 2);
+    c[0] = x.x; c[1] = x.y;
+    s[0] = y.x; s[1] = y.y;
+  }
+  if (!in) {
+#pragma unroll
+    for (int e = 0; e < n; ++e) c[e] = s[e] = NAN;
+  }
+}
+
+// The cosines and sines of pairs p .. p + n of token t, n 2 or a multiple of 4 that p is a
+// multiple of.
 template <int kRotDim, int n>
 __device__ __forceinline__ void load_turns(const QkvArgs& a, int t, int p, float* c, float* s) {
-  constexpr int kHalf = kRotDim / 2;
+  constexpr int kHalf = kRotDim / 2, kStep = n % 4 == 0 ? 4 : 2;
+  auto axis_of = [&](int pair) __attribute__((always_inline)) {
+    return (pair >= a.axis_end[0]) + (pair >= a.axis_end[1]) + (pair >= a.axis_end[2]);
+  };
   if (a.axis_end[0] >= kHalf) {   // one axis
     const int pos = a.positions[t];
-    const bool in = (unsigned)pos < (unsigned)a.table_len;
-    const float* at = a.table + (size_t)(in ? pos : 0) * kRotDim + p;
-    if constexpr (n % 4 == 0) {
 #pragma unroll
-      for (int e = 0; e < n; e += 4) {
-        const float4 x = *reinterpret_cast<const float4*>(at + e);
-        const float4 y = *reinterpret_cast<const float4*>(at + kHalf + e);
-        c[e] = x.x; c[e + 1] = x.y; c[e + 2] = x.z; c[e + 3] = x.w;
-        s[e] = y.x; s[e + 1] = y.y; s[e + 2] = y.z; s[e + 3] = y.w;
-      }
+    for (int e = 0; e < n; e += kStep) load_turns_at<kRotDim, kStep>(a, pos, p + e, c + e, s + e);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < n; e += kStep) {
+    const int axis = axis_of(p + e);
+    if (axis == axis_of(p + e + kStep - 1)) {   // no section ends among them
+      load_turns_at<kRotDim, kStep>(a, a.positions[(size_t)axis * a.num_tokens + t], p + e, c + e,
+                                    s + e);
     } else {
-      const float2 x = *reinterpret_cast<const float2*>(at);
-      const float2 y = *reinterpret_cast<const float2*>(at + kHalf);
-      c[0] = x.x; c[1] = x.y;
-      s[0] = y.x; s[1] = y.y;
-    }
-    if (!in) {
 #pragma unroll
-      for (int e = 0; e < n; ++e) c[e] = s[e] = NAN;
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < n; ++e) {
-      const int axis = (p + e >= a.axis_end[0]) + (p + e >= a.axis_end[1]) +
-                       (p + e >= a.axis_end[2]);
-      const int pos = a.positions[(size_t)axis * a.num_tokens + t];
-      const bool in = (unsigned)pos < (unsigned)a.table_len;
-      const float* at = a.table + (size_t)(in ? pos : 0) * kRotDim + p + e;
-      c[e] = in ? at[0] : NAN;
-      s[e] = in ? at[kHalf] : NAN;
+      for (int i = e; i < e + kStep; ++i) {
+        const int pos = a.positions[(size_t)axis_of(p + i) * a.num_tokens + t];
+        const bool in = (unsigned)pos < (unsigned)a.table_len;
+        const float* at = a.table + (size_t)(in ? pos : 0) * kRotDim + p + i;
+        c[i] = in ? at[0] : NAN;
+        s[i] = in ? at[kHalf] : NAN;
+      }
     }
   }
 }
