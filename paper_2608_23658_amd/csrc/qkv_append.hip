@@ -19,15 +19,15 @@
 
 namespace kvattn {
 
-// One K (g < num_kv_heads) or V head of run k.
+// Heads h0 .. h1 of run k: K heads, then V heads.
 template <int ESZ, int D, int kRotDim, bool kEven>
-__device__ __forceinline__ void kv_rows(const QkvArgs& a, int k, int g, uint4* stage) {
-  using R = TileRows<ESZ, D, kRotDim * ESZ / 64, kEven>;
+__device__ __forceinline__ void kv_rows(const QkvArgs& a, int k, int h0, int h1,
+                                        uint4* stage) {
+  using R = LaneRows<ESZ, D, kRotDim, kEven, true>;
+  constexpr int kRows = kRunTokens * R::kLanes / kWave;   // rows of a lane
+  constexpr int kN = kRows * R::kPer;                     // its 16-byte pieces
   const int lane = threadIdx.x % kWave;
-  const int row = lane / 16;
   const int hkv = a.num_kv_heads;
-  const bool is_v = g >= hkv;
-  if (is_v) g -= hkv;
   constexpr size_t kTile = (size_t)kRunTokens * D * ESZ;
 
   // Lane l looks at token 16 (k - 1) + l; the run's are among lanes 1 .. 31.
@@ -49,110 +49,141 @@ __device__ __forceinline__ void kv_rows(const QkvArgs& a, int k, int g, uint4* s
   const int rank = __popcll(run & ((1ull << lane) - 1));
   const int packed = __builtin_amdgcn_ds_permute((mine ? rank : kWave - 1) * 4, lane);
 
-  R rows;
-  const uint8_t* weight = is_v ? nullptr : a.k_weight;
-  const uint8_t* src = is_v ? a.v : a.k;
-  const size_t stride = is_v ? a.v_stride : a.k_stride;
+  const int piece = lane % R::kLanes;
+  const bool any_k = h0 < hkv;
+  float w[R::kElems];
+  if (any_k && a.k_weight) R::weights(a.k_weight, piece, w);
   for (int from = 0; from < n; from += kRunTokens) {   // 16 at a time, once where in order
+    int tok[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const int i16 = min(from + lane / R::kLanes + r * (kWave / R::kLanes), n - 1);
+      tok[r] = kRunTokens * (k - 1) + __shfl(packed, i16, kWave);
+    }
+    auto load = [&](int h, uint4 (&x)[kN]) __attribute__((always_inline)) {
+      const uint8_t* src = h < hkv ? a.k + (size_t)h * (D * ESZ) : a.v + (size_t)(h - hkv) * (D * ESZ);
+      const size_t stride = h < hkv ? a.k_stride : a.v_stride;
+#pragma unroll
+      for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int p = 0; p < R::kPer; ++p)
+          x[r * R::kPer + p] = load_nt(
+              reinterpret_cast<const uint4*>(src + (size_t)tok[r] * stride) + piece + R::kLanes * p);
+    };
+    uint4 ahead[kN];
+    load(h0, ahead);
+    float c[kRows][R::kPairs], s[kRows][R::kPairs];
+    if (any_k) {
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) R::turns(a, tok[r], piece, c[r], s[r]);
+    }
     const int i16 = from + lane % 16;
     const bool live = i16 < n;
-    const int l = __shfl(packed, live ? i16 : from, kWave);
-    const int my_slot = __shfl(slot, l, kWave), tok = kRunTokens * (k - 1) + l;
+    const int my_slot = __shfl(slot, __shfl(packed, live ? i16 : from, kWave), kWave);
     const int s0 = __builtin_amdgcn_readfirstlane(my_slot);
     const bool whole =
         n - from >= kRunTokens && s0 % kRunTokens == 0 && __all(my_slot == s0 + lane % 16);
-    uint4 raw[R::kN];
-#pragma unroll
-    for (int i = 0; i < R::kN; ++i)
-      raw[i] = load_nt(reinterpret_cast<const uint4*>(src + (size_t)tok * stride +
-                                                      (size_t)g * (D * ESZ)) + 4 * i + row);
-    uint8_t* tile = a.kv + (size_t)(my_slot / kRunTokens) * (2 * (size_t)hkv * kTile) +
-                    (size_t)((is_v ? hkv : 0) + g) * kTile;
+    uint8_t* block = a.kv + (size_t)(my_slot / kRunTokens) * (2 * (size_t)hkv * kTile);
     const int in_block = my_slot % kRunTokens;
-    if (!is_v) {
-      if (weight) rows.load_weight(weight);
-      rows.load(a, tok);
-      float x[R::kElems];
+
+    for (int h = h0; h < h1; ++h) {
+      const bool is_v = h >= hkv;
+      uint8_t* tile = block + (size_t)h * kTile;
+      uint4 raw[kN];
 #pragma unroll
-      for (int i = 0; i < R::kN; ++i) R::P::widen(raw[i], x + i * R::kVec);
-      if (weight) rows.norm(x, a.eps);
-      rows.rotate(x);
-      if (live) {
-        uint4* to = reinterpret_cast<uint4*>(tile);
+      for (int i = 0; i < kN; ++i) raw[i] = ahead[i];
+      if (h + 1 < h1) load(h + 1, ahead);
+      if (!is_v) {
 #pragma unroll
-        for (int i = 0; i < R::kN; ++i)
-          to[(4 * i + row) * kRunTokens + in_block] = R::P::narrow(x + i * R::kVec);
+        for (int r = 0; r < kRows; ++r) {
+          float x[R::kElems];
+#pragma unroll
+          for (int p = 0; p < R::kPer; ++p) R::P::widen(raw[r * R::kPer + p], x + p * R::kVec);
+          if (a.k_weight) R::norm(x, w, a.eps);
+          R::rotate(x, piece, c[r], s[r]);
+#pragma unroll
+          for (int p = 0; p < R::kPer; ++p) raw[r * R::kPer + p] = R::P::narrow(x + p * R::kVec);
+        }
       }
-    } else if (whole) {
-      // Through LDS (rows padded against conflicts): a dim's 16 slots leave as 16-byte pieces.
+      // Through LDS (rows padded against conflicts) from rows along the lanes to the tile's order.
       constexpr int kRowU4 = D * ESZ / 16 + 1, kVec = R::kVec, kParts = kRunTokens / kVec;
 #pragma unroll
-      for (int i = 0; i < R::kN; ++i) stage[lane % 16 * kRowU4 + 4 * i + row] = raw[i];
+      for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int p = 0; p < R::kPer; ++p)
+          stage[(lane / R::kLanes + r * (kWave / R::kLanes)) * kRowU4 + piece + R::kLanes * p] =
+              raw[r * R::kPer + p];
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
+      if (is_v && whole) {   // a dim's 16 slots leave as 16-byte pieces
 #pragma unroll
-      for (int i = 0; i < R::kN; ++i) {
-        const int idx = i * kWave + lane, j = idx / kParts, part = idx % kParts;
-        uint32_t w[4];
-        if constexpr (ESZ == 2) {
-          const uint16_t* in = reinterpret_cast<const uint16_t*>(stage) + j;
+        for (int i = 0; i < kN; ++i) {
+          const int idx = i * kWave + lane, j = idx / kParts, part = idx % kParts;
+          uint32_t v[4];
+          if constexpr (ESZ == 2) {
+            const uint16_t* in = reinterpret_cast<const uint16_t*>(stage) + j;
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            w[e] = in[(part * 8 + 2 * e) * kRowU4 * 8] |
-                   (uint32_t)in[(part * 8 + 2 * e + 1) * kRowU4 * 8] << 16;
-        } else {
-          const uint32_t* in = reinterpret_cast<const uint32_t*>(stage) + j;
+            for (int e = 0; e < 4; ++e)
+              v[e] = in[(part * 8 + 2 * e) * kRowU4 * 8] |
+                     (uint32_t)in[(part * 8 + 2 * e + 1) * kRowU4 * 8] << 16;
+          } else {
+            const uint32_t* in = reinterpret_cast<const uint32_t*>(stage) + j;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = in[(part * 4 + e) * kRowU4 * 4];
+            for (int e = 0; e < 4; ++e) v[e] = in[(part * 4 + e) * kRowU4 * 4];
+          }
+          reinterpret_cast<uint4*>(tile)[idx] = make_uint4(v[0], v[1], v[2], v[3]);
         }
-        reinterpret_cast<uint4*>(tile)[idx] = make_uint4(w[0], w[1], w[2], w[3]);
+      } else if (live) {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+          const int chunk = 4 * i + lane / 16;
+          const uint4 x = stage[lane % 16 * kRowU4 + chunk];
+          if (!is_v) {
+            reinterpret_cast<uint4*>(tile)[chunk * kRunTokens + in_block] = x;
+          } else {
+            const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+              const int at = (chunk * kVec + e) * kRunTokens + in_block;
+              if constexpr (ESZ == 2)
+                reinterpret_cast<uint16_t*>(tile)[at] = (uint16_t)(u[e / 2] >> (16 * (e % 2)));
+              else
+                reinterpret_cast<uint32_t*>(tile)[at] = u[e];
+            }
+          }
+        }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-    } else if (live) {
-#pragma unroll
-      for (int i = 0; i < R::kN; ++i) {
-        const uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-        const int j0 = (4 * i + row) * R::kVec;
-        if constexpr (ESZ == 2) {
-          uint16_t* v = reinterpret_cast<uint16_t*>(tile);
-#pragma unroll
-          for (int e = 0; e < R::kVec; ++e)
-            v[(j0 + e) * kRunTokens + in_block] = (uint16_t)(u[e / 2] >> (16 * (e % 2)));
-        } else {
-          uint32_t* v = reinterpret_cast<uint32_t*>(tile);
-#pragma unroll
-          for (int e = 0; e < R::kVec; ++e) v[(j0 + e) * kRunTokens + in_block] = u[e];
-        }
-      }
     }
   }
 }
 
 template <int ESZ, int D, int kRotDim, bool kEven>
 __global__ __launch_bounds__(kQkvWaves * kWave) void qkv_append_kernel(QkvArgs a, int kv_wgs,
-                                                                       int groups, int per_wave) {
+                                                                       QkvSplit kv, QkvSplit q) {
   __shared__ uint4 stage[kQkvWaves][kRunTokens * (D * ESZ / 16 + 1)];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   if ((int)blockIdx.x < kv_wgs) {
-    const int task = blockIdx.x * kQkvWaves + wave, heads = 2 * a.num_kv_heads;
-    kv_rows<ESZ, D, kRotDim, kEven>(a, task / heads, task % heads, stage[wave]);
+    const int h0 = (blockIdx.x % kv.groups * kQkvWaves + wave) * kv.per_wave;
+    const int h1 = min(2 * a.num_kv_heads, h0 + kv.per_wave);
+    if (h0 < h1) kv_rows<ESZ, D, kRotDim, kEven>(a, blockIdx.x / kv.groups, h0, h1, stage[wave]);
   } else {
-    q_rows<ESZ, D, kRotDim, kEven>(a, blockIdx.x - kv_wgs, groups, per_wave);
+    q_rows<ESZ, D, kRotDim, kEven>(a, blockIdx.x - kv_wgs, q.groups, q.per_wave);
   }
 }
 
 template <int ESZ, int D, int kRotDim, bool kEven>
 static hipError_t launch_qkv_t(const QkvArgs& a) {
+  const int runs = (int)(((long long)a.num_tokens + kRunTokens - 1) / kRunTokens);
+  const QkvSplit q = qkv_split(runs, a.num_q_heads);
   // a token's run may be the one after that of its place in the list
-  const long long runs = ((long long)a.num_tokens + kRunTokens - 1) / kRunTokens + 1;
-  const long long kv_wgs = (runs * 2 * a.num_kv_heads + kQkvWaves - 1) / kQkvWaves;
-  const QkvSplit s = qkv_split(a.num_tokens, a.num_q_heads);
-  if (kv_wgs + s.workgroups > 0x7fffffffLL / kQkvWaves) return hipErrorInvalidValue;
+  const QkvSplit kv = qkv_split(runs + 1, 2 * a.num_kv_heads);
+  if (kv.workgroups + q.workgroups > 0x7fffffffLL / kQkvWaves) return hipErrorInvalidValue;
   trace_before(a.stream, "qkv_append");
   hipLaunchKernelGGL((qkv_append_kernel<ESZ, D, kRotDim, kEven>),
-                     dim3((unsigned)(kv_wgs + s.workgroups)), dim3(kQkvWaves * kWave), 0, a.stream,
-                     a, (int)kv_wgs, s.groups, s.per_wave);
+                     dim3((unsigned)(kv.workgroups + q.workgroups)), dim3(kQkvWaves * kWave), 0,
+                     a.stream, a, (int)kv.workgroups, kv, q);
   trace_after(a.stream);
   return hipGetLastError();
 }

@@ -12,7 +12,7 @@ namespace kvattn {
 template <int ESZ, int D, int kRotDim, bool kEven>
 struct KeyPrep {
   static constexpr bool kOn = true;
-  using R = LaneRows<ESZ, D, kRotDim, kEven>;
+  using R = LaneRows<ESZ, D, kRotDim, kEven, false>;
   const QkvArgs& a;
 
   // The lane's pieces x of token t, the first of them the row's piece-th.
@@ -45,7 +45,7 @@ template <int ESZ, int D, int kRotDim, bool kEven>
 static hipError_t launch_qkv_fp8_t(const QkvArgs& a) {
   const int win = append_window(a.num_tokens);
   const long long append_wgs = ((long long)a.num_tokens + win - 1) / win * a.num_kv_heads;
-  const QkvSplit rows = qkv_split(a.num_tokens, a.num_q_heads);
+  const QkvSplit rows = qkv_split(((long long)a.num_tokens + kRunTokens - 1) / kRunTokens, a.num_q_heads);
   const long long blocks = append_wgs + rows.workgroups;
   if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
   auto kernel = win == kFewWindow    ? qkv_append_fp8_kernel<ESZ, D, kRotDim, kEven, kFewWindow>

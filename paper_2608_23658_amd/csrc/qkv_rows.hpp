@@ -1,5 +1,4 @@
-// Norm and rotation of q and k rows in registers, in the two orders that the kernels hold
-// them in.
+// Norm and rotation of q and k rows in registers.
 #pragma once
 
 #include <type_traits>
@@ -107,31 +106,34 @@ __device__ __forceinline__ void load_turns(const QkvArgs& a, int t, int p, float
 
 // ---- rows along the lanes ----
 // A row's 16-byte pieces lie in 8 or 16 neighbouring lanes (512 bytes: two in each of 16),
-// so that rows are read and written as they lie. kRotDim 0: no rotation.
-template <int ESZ, int D, int kRotDim, bool kEven>
+// so that rows are read and written as they lie. kRotDim 0: no rotation. kPairsIn: a row
+// of 256 bytes whose pairs are its halves has two pieces in each of 8 lanes, so that a
+// lane has both of a pair and a pair's cosine and sine are read once.
+template <int ESZ, int D, int kRotDim, bool kEven, bool kPairsIn>
 struct LaneRows {
   using P = QkvPieces<ESZ>;
   static constexpr int kVec = P::kVec, kCh = D / kVec;
-  static constexpr int kPer = kCh > 16 ? kCh / 16 : 1;   // pieces of a row in a lane
-  static constexpr int kLanes = kCh / kPer;              // lanes of a row
+  static constexpr bool kHalves = kPairsIn && !kEven && kRotDim == D && kCh == 16;
+  static constexpr int kPer = kHalves || kCh > 16 ? 2 : 1;   // pieces of a row in a lane
+  static constexpr int kLanes = kCh / kPer;                  // lanes of a row, pieces apart
   static constexpr int kElems = kPer * kVec;
   static constexpr int kOff = kRotDim / 2 / kVec;        // pieces between the two of a pair
-  static constexpr bool kInLane = kEven || kOff >= 16;   // both of a pair in a lane
+  static constexpr bool kInLane = kEven || kOff == kLanes;   // both of a pair in a lane
   static constexpr int kPairs = kRotDim == 0 ? 1 : kInLane ? kElems / 2 : kVec;
 
-  // The cosines and sines that a lane with pieces piece, piece + 16 needs of token t.
+  // The cosines and sines that a lane with pieces piece, piece + kLanes needs of token t.
   static __device__ __forceinline__ void turns(const QkvArgs& a, int t, int piece, float (&c)[kPairs],
                                                float (&s)[kPairs]) {
     if constexpr (kRotDim > 0) {
 #pragma unroll
       for (int p = 0; p < kPer; ++p) {
         if constexpr (kEven) {
-          if ((piece + 16 * p) * kVec < kRotDim)
-            load_turns<kRotDim, kVec / 2>(a, t, (piece + 16 * p) * (kVec / 2), c + p * (kVec / 2),
+          if ((piece + kLanes * p) * kVec < kRotDim)
+            load_turns<kRotDim, kVec / 2>(a, t, (piece + kLanes * p) * (kVec / 2), c + p * (kVec / 2),
                                           s + p * (kVec / 2));
         } else if constexpr (kInLane) {
           if (p < kPer / 2)
-            load_turns<kRotDim, kVec>(a, t, (piece + 16 * p) * kVec, c + p * kVec, s + p * kVec);
+            load_turns<kRotDim, kVec>(a, t, (piece + kLanes * p) * kVec, c + p * kVec, s + p * kVec);
         } else if (p == 0 && piece < 2 * kOff) {
           load_turns<kRotDim, kVec>(a, t, piece % kOff * kVec, c, s);
         }
@@ -142,7 +144,7 @@ struct LaneRows {
                                                  float (&w)[kElems]) {
 #pragma unroll
     for (int p = 0; p < kPer; ++p)
-      P::widen(reinterpret_cast<const uint4*>(weight)[piece + 16 * p], w + p * kVec);
+      P::widen(reinterpret_cast<const uint4*>(weight)[piece + kLanes * p], w + p * kVec);
   }
   // x * rsqrt(mean(x^2) + eps) * w
   static __device__ __forceinline__ void norm(float* x, const float (&w)[kElems], float eps) {
@@ -170,7 +172,7 @@ struct LaneRows {
     if constexpr (kEven) {
 #pragma unroll
       for (int p = 0; p < kPer; ++p)
-        if ((piece + 16 * p) * kVec < kRotDim) {
+        if ((piece + kLanes * p) * kVec < kRotDim) {
 #pragma unroll
           for (int m = 0; m < kVec / 2; ++m)
             turn(x[p * kVec + 2 * m], x[p * kVec + 2 * m + 1], c[p * (kVec / 2) + m],
@@ -191,85 +193,11 @@ struct LaneRows {
   }
 };
 
-// ---- rows across the lanes, in the order of the cache's K tile ----
-// A wavefront has one head's rows of 16 tokens: lane l has token l % 16 and, of its row's
-// 16-byte chunks, chunk 4 i + l / 16 in register i. So a register's 64 lanes are 1 KiB of
-// a K tile as it lies in the cache; a row's sum is a lane's own and one exchange between the
-// four lanes of a row; and the two dims of a pair, half the rotated dims apart, are a whole
-// number of registers apart in the same lane (32 rotated dims of bf16 excepted: there they
-// are two lanes of a row).
-// kRot: registers of rotated chunks (0: no rotation). kEven: pairs are adjacent dims.
-template <int ESZ, int D, int kRot, bool kEven>
-struct TileRows {
-  using P = QkvPieces<ESZ>;
-  static constexpr int kVec = 16 / ESZ;            // elements per chunk
-  static constexpr int kN = D / kVec / 4;          // chunks per lane
-  static constexpr int kElems = kN * kVec;
-  static constexpr int kRotDim = kRot * 4 * kVec;
-  static constexpr bool kSwap = kRot == 1 && !kEven;   // a pair is in two lanes
-  static constexpr int kPairs = kSwap ? kVec : kRot * kVec / 2;   // cosines per lane
-  static constexpr int kRun = kEven && kRot ? kVec / 2 : kVec;    // of them in a row of the table
-  static_assert(kRot <= kN && (kRot % 2 == 0 || kRot == 1), "whole registers");
-
-  float cs[kPairs ? kPairs : 1], sn[kPairs ? kPairs : 1];
-  float w[kElems];   // the norm's weight
-
-  static __device__ __forceinline__ int row() { return threadIdx.x % kWave / 16; }
-
-  // First pair of the lane's i-th run of kRun pairs.
-  static __device__ __forceinline__ int first_pair(int i) {
-    return kSwap ? row() % 2 * kVec : (4 * i + row()) * kRun;
-  }
-
-  // The cosines and sines of token t's positions.
-  __device__ __forceinline__ void load(const QkvArgs& a, int t) {
-    if constexpr (kRot > 0) {
-#pragma unroll
-      for (int i = 0; i < kPairs / kRun; ++i)
-        load_turns<kRotDim, kRun>(a, t, first_pair(i), cs + i * kRun, sn + i * kRun);
-    }
-  }
-
-  __device__ __forceinline__ void load_weight(const uint8_t* weight) {
-    if (!weight) return;
-#pragma unroll
-    for (int i = 0; i < kN; ++i)
-      P::widen(reinterpret_cast<const uint4*>(weight)[4 * i + row()], w + i * kVec);
-  }
-
-  // x * rsqrt(mean(x^2) + eps) * w, in fp32
-  __device__ __forceinline__ void norm(float (&x)[kElems], float eps) const {
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < kElems; ++e) sum = fmaf(x[e], x[e], sum);
-    const float by = rsqrtf(fmaf(cross_row_sum(sum), 1.f / D, eps));
-#pragma unroll
-    for (int e = 0; e < kElems; ++e) x[e] = x[e] * by * w[e];
-  }
-
-  __device__ __forceinline__ void rotate(float (&x)[kElems]) const {
-    if constexpr (kSwap) {
-      const bool second = row() >= 2;
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const float other = __shfl_xor(x[e], 32, kWave);
-        x[e] = fmaf(x[e], cs[e], second ? other * sn[e] : -other * sn[e]);
-      }
-    } else if constexpr (kEven) {
-#pragma unroll
-      for (int p = 0; p < kPairs; ++p) turn(x[2 * p], x[2 * p + 1], cs[p], sn[p]);
-    } else {
-#pragma unroll
-      for (int p = 0; p < kPairs; ++p) turn(x[p], x[p + kPairs], cs[p], sn[p]);
-    }
-  }
-};
-
 // The q rows of workgroup wg, of (runs x groups of heads): per_wave heads a wavefront, the
 // next one's rows on their way while one's are computed.
 template <int ESZ, int D, int kRotDim, bool kEven>
 __device__ __forceinline__ void q_rows(const QkvArgs& a, int wg, int groups, int per_wave) {
-  using R = LaneRows<ESZ, D, kRotDim, kEven>;
+  using R = LaneRows<ESZ, D, kRotDim, kEven, true>;
   constexpr int kRows = kRunTokens * R::kLanes / kWave;   // rows of a lane
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -287,7 +215,7 @@ __device__ __forceinline__ void q_rows(const QkvArgs& a, int wg, int groups, int
         x[r * R::kPer + p] =
             load_nt(reinterpret_cast<const uint4*>(
                         a.q + (size_t)min(token(r), a.num_tokens - 1) * a.q_stride +
-                        (size_t)h * (D * ESZ)) + piece + 16 * p);
+                        (size_t)h * (D * ESZ)) + piece + R::kLanes * p);
   };
   uint4 next[kRows * R::kPer];
   load(h0, next);
@@ -312,7 +240,7 @@ __device__ __forceinline__ void q_rows(const QkvArgs& a, int wg, int groups, int
       if (token(r) < a.num_tokens) {
         uint4* to = reinterpret_cast<uint4*>(a.q_out + ((size_t)token(r) * hq + h) * (D * ESZ));
 #pragma unroll
-        for (int p = 0; p < R::kPer; ++p) to[piece + 16 * p] = R::P::narrow(x + p * R::kVec);
+        for (int p = 0; p < R::kPer; ++p) to[piece + R::kLanes * p] = R::P::narrow(x + p * R::kVec);
       }
     }
   }
@@ -323,8 +251,7 @@ struct QkvSplit {
   int per_wave, groups;   // heads of a wavefront, workgroups of a run
   long long workgroups;
 };
-inline QkvSplit qkv_split(int tokens, int heads) {
-  const long long runs = ((long long)tokens + kRunTokens - 1) / kRunTokens;
+inline QkvSplit qkv_split(long long runs, int heads) {
   QkvSplit s;
   s.per_wave = runs * heads > 8192 ? 8 : runs * heads > 4096 ? 4 : runs * heads > 2048 ? 2 : 1;
   s.groups = (heads + kQkvWaves * s.per_wave - 1) / (kQkvWaves * s.per_wave);
