@@ -326,8 +326,8 @@ typedef struct {
  * scale * log2(e) must be finite. With a window, what is read of a sequence is the last
  * window tokens: table entries of blocks wholly before them are not read, and what the
  * window's first block holds before its first token has no effect, NaN included. A workspace
- * for min(max_seq_len, window + 15) tokens is enough. The cap is within 2^-21 of it of
- * softcap * tanh (near zero within 2^-21 of the value itself). A sequence's bits depend on
+ * for min(max_seq_len, window + 15) tokens is enough. A capped score is off by at
+ * most softcap * 2^-21 (in fp32, by what the library's tanh is). A sequence's bits depend on
  * itself, scoring and scale alone.
  * Supported: as kvattn_decode (bf16 with head_dim 64 or 128, fp32 with 64) and
  * kvattn_decode_fp8. */

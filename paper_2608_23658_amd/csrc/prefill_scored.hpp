@@ -1,4 +1,25 @@
-// Chunked prefill with scores that are capped, biased by distance or cut to a window.
+// Chunked prefill with scores that are capped, biased by distance or cut to a window: the
+// tile pipeline of prefill_tile.hpp, with scores made by ModScore.
+//
+// The plan cuts a tile's key steps to those that its rows' windows reach (an even first step, as
+// the pipeline takes steps by twos) and prices items by what is left. The matrix
+// work of a step takes a little longer than its softmax beside it, so what a score costs more shows:
+//   a window's masks are made only in steps that a window begins in;
+//   a bias is one multiply-add in the softmax's own slots (fma(dot, scale, bias - reference));
+//   a cap comes before the mask and cannot hide there. Where all of a wavefront's products of a
+//     step are under half the cap it is a polynomial of four multiply-adds a score, else an
+//     exponential, a reciprocal and three more operations.
+// A bias or a cap walks a tile's keys from the last to the first: a steep slope's largest
+// scores then come first, and the softmax's reference moves once instead of at every step.
+// Each kind of scores has kernels of its own, since one that asks for its kind at every score
+// needs more registers than there are and spilled. Per call, plain prefill / window of 1024 /
+// bias / cap / cap and bias (32 query heads over 8):
+//   8192 rows over 24576                    3447 /  222 / 3254 / 4355 / 4210 us
+//   4096 rows over 12288                     909 /  115 /  831 / 1115 / 1073 us
+//   201 rows over 6150                      51.1 / 42.0 / 50.9 / 62.6 / 59.3 us
+//   2048 rows over 6144 and 64 of 1024 to
+//     8192, 8 bits                           347 /   78 /  343 /  426 /  424 us
+// (the biased ones gain by the order of the keys: near ones hold a row's largest scores.)
 
 #pragma once
 

@@ -4,8 +4,20 @@
 // block id; Section 2: blocks of fixed size).
 //
 // The first workgroups have K and V, a wavefront one head's K or V of a run of tokens; the
-// others have q, some heads of a run of 16 tokens one after another, so that the cosines and
-// sines are read once. Every row is read once and written once.
+// others have q. A wavefront has some heads of a run of 16 tokens one after another, the next
+// one's rows on their way while one's are computed, so that the cosines and sines are read
+// once and no wavefront waits for each of its loads in turn. Every row is read once and written
+// once; about 10 operations a value leave HBM as the bound. Rows are read along the lanes, 128
+// bytes or more of each at a time, and K and V turned through LDS into the tiles' order.
+// 8192 tokens in order, 128 dims, bf16, inputs not in a cache; copying as many bytes takes 42 us:
+//   a head's rows in the tile's order in registers, one head a wavefront,
+//     V's dims stored one by one                                                   77.0 us
+//   q along the lanes with loads ahead, K and V by blocks, V through LDS           57.2
+//   K along the lanes and heads one after another with loads ahead too             51.5
+//   both dims of a pair in a lane (LaneRows::kPairsIn)                             43.5
+// (32 query heads over 8; 16 over 16 83.4 -> 43.2). 256 scattered tokens: 15.1 us, or 10.3 in a
+// graph with the inputs in the caches. There each of V's 2-byte elements goes into a 32-byte
+// run of its own, a quarter of a million of them.
 //
 // A run of K or V is the tokens of one block where tokens follow each other in slot order, so
 // that a block is written whole by one wavefront wherever a chunk begins in it; tokens
@@ -61,7 +73,8 @@ __device__ __forceinline__ void kv_rows(const QkvArgs& a, int k, int h0, int h1,
       tok[r] = kRunTokens * (k - 1) + __shfl(packed, i16, kWave);
     }
     auto load = [&](int h, uint4 (&x)[kN]) __attribute__((always_inline)) {
-      const uint8_t* src = h < hkv ? a.k + (size_t)h * (D * ESZ) : a.v + (size_t)(h - hkv) * (D * ESZ);
+      const uint8_t* src =
+          h < hkv ? a.k + (size_t)h * (D * ESZ) : a.v + (size_t)(h - hkv) * (D * ESZ);
       const size_t stride = h < hkv ? a.k_stride : a.v_stride;
 #pragma unroll
       for (int r = 0; r < kRows; ++r)

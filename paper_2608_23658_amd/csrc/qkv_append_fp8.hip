@@ -1,6 +1,11 @@
 // The norm, rotation and cache write of qkv_append.hip over a cache in 8 bits: K rows
 // are scaled and rounded from the fp32 values that the rotation gives. One launch: the
-// first workgroups append K and V as append_fp8.hpp does, the others have the q rows.
+// first workgroups append K and V as append_fp8.hpp does, the others have the q rows. A K
+// row is normed and rotated in the lanes that hold it for its scale.
+// 8192 tokens in order, 32 query heads over 8 of 128, bf16, inputs not in a cache: 53.6 us, where
+// copying as many bytes takes 38.5; 4096 tokens of 64 over 8: 39.7, copy 32.9, and 36.5 in a
+// graph. With K's pairs looked up value by value it was 93.8 and 73.6. 256 scattered tokens: 16.2 us
+// (25.4), a chain of latencies: slots, exponents and positions, rows and table, codes.
 
 #include "append_fp8.hpp"
 #include "launch.hpp"
@@ -45,7 +50,8 @@ template <int ESZ, int D, int kRotDim, bool kEven>
 static hipError_t launch_qkv_fp8_t(const QkvArgs& a) {
   const int win = append_window(a.num_tokens);
   const long long append_wgs = ((long long)a.num_tokens + win - 1) / win * a.num_kv_heads;
-  const QkvSplit rows = qkv_split(((long long)a.num_tokens + kRunTokens - 1) / kRunTokens, a.num_q_heads);
+  const QkvSplit rows =
+      qkv_split(((long long)a.num_tokens + kRunTokens - 1) / kRunTokens, a.num_q_heads);
   const long long blocks = append_wgs + rows.workgroups;
   if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
   auto kernel = win == kFewWindow    ? qkv_append_fp8_kernel<ESZ, D, kRotDim, kEven, kFewWindow>
