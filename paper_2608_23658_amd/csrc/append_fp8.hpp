@@ -224,17 +224,18 @@ __device__ __forceinline__ void append_fp8(
       if (prepared) {
         if constexpr (Prep::kOn) {
 #pragma unroll
-          for (int e = 0; e < kLoads * kVec; ++e) amax = max(amax, finite_bits(__float_as_uint(y[e])));
+          for (int e = 0; e < kLoads * kVec; ++e)
+            amax = max(amax, finite_bits(__float_as_uint(y[e])));
         }
       } else {
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i)
+        for (int i = 0; i < kLoads; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t w = (&x[i].x)[e];
-          amax = max(amax, finite_bits(ESZ == 2 ? w & 0xffff0000u : w));
-          if (ESZ == 2) amax = max(amax, finite_bits(w << 16));
-        }
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t w = (&x[i].x)[e];
+            amax = max(amax, finite_bits(ESZ == 2 ? w & 0xffff0000u : w));
+            if (ESZ == 2) amax = max(amax, finite_bits(w << 16));
+          }
       }
       amax = wave_umax(amax);
     }

@@ -419,7 +419,8 @@ void decode_split_kernel(
       const int t0 = s0 + wave * part_tokens;
       if constexpr (kFp8)
         walk_fp8<D, G, kAhead>(tiles8, reinterpret_cast<const uint16_t*>(q_row), bt, num_blocks,
-                               t0, min(s1, t0 + part_tokens), score, o_lds[0], ml_lds[0], h0, L - 1, lo);
+                               t0, min(s1, t0 + part_tokens), score, o_lds[0], ml_lds[0], h0,
+                               L - 1, lo);
       else
         walk_bf16<D, G, kTwo, kAhead>(tiles, reinterpret_cast<const uint16_t*>(q_row), bt,
                                       num_blocks, t0, min(s1, t0 + part_tokens), score, o_lds[0],
@@ -452,7 +453,8 @@ void decode_split_kernel(
         const int t0 = s0 + p * part_tokens;
         if constexpr (kFp8)
           walk_fp8<D, G, kAhead>(tiles8, reinterpret_cast<const uint16_t*>(q_row), bt, num_blocks,
-                                 t0, min(s1, t0 + part_tokens), score, o_lds[p], ml_lds[p], h0, L - 1, lo);
+                                 t0, min(s1, t0 + part_tokens), score, o_lds[p], ml_lds[p], h0,
+                                 L - 1, lo);
         else
           walk_bf16<D, G, kTwo, kAhead>(tiles, reinterpret_cast<const uint16_t*>(q_row), bt,
                                         num_blocks, t0, min(s1, t0 + part_tokens), score, o_lds[p],

@@ -285,7 +285,8 @@ __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
     step_ids(tb, id_a);
     load_step<true>(tiles, id_a, lane, v_lane, k_a, v_a);
     // only a walk's first step can hold tokens before lo: here, and not in the loop, where a
-    // branch would keep later loads from being counted (1 sequence of 3971 with a cap: 14.2 -> 13.6 us)
+    // branch would keep later loads from being counted (1 sequence of 3971 with a cap: 14.2 ->
+    // 13.6 us)
     if (Score::kOn && tb < lo) cut(tb, v_a);
     for (;;) {
       if (tb + S::kTile >= t1) {

@@ -265,7 +265,8 @@ __device__ __forceinline__ void prefill_tile(
       bits = __builtin_amdgcn_readfirstlane(bits);
       asm volatile("" : "+s"(bits));   // compared each time, no mask kept
     }
-    return bits == 0xf && (at_step(step) + 1) * kKeys <= L && (!Score::kOn || at_step(step) * kKeys >= lo);
+    return bits == 0xf && (at_step(step) + 1) * kKeys <= L &&
+           (!Score::kOn || at_step(step) * kKeys >= lo);
   };
 
   const int wave_pos0 = c + row0;   // position of the wave's first row
@@ -684,9 +685,9 @@ __device__ __forceinline__ void prefill_row(
   if constexpr (Score::kOn) lo = score.first_key(it.L - 1);
   if (wave < parts) {
     const int t0 = i0 + wave * per;
-    walk_bf16<kD, G, false, false>(tiles, q + row, block_table + (size_t)it.s * max_blocks, num_blocks,
-                            t0, min(i1, t0 + per), score, o_lds[wave], ml_lds[wave], g * G, it.L - 1,
-                            lo);
+    walk_bf16<kD, G, false, false>(tiles, q + row, block_table + (size_t)it.s * max_blocks,
+                                   num_blocks, t0, min(i1, t0 + per), score, o_lds[wave],
+                                   ml_lds[wave], g * G, it.L - 1, lo);
   }
   __syncthreads();
   for (int e = threadIdx.x; e < G * kD; e += kThreads) {

@@ -657,7 +657,8 @@ __device__ __forceinline__ void prefill_row_fp8(
   if (wave < parts) {
     const int t0 = i0 + wave * per;
     walk_fp8<kD, G, false>(tiles, q + row, block_table + (size_t)it.s * max_blocks, num_blocks, t0,
-                           min(i1, t0 + per), score, o_lds[wave], ml_lds[wave], g * G, it.L - 1, lo);
+                           min(i1, t0 + per), score, o_lds[wave], ml_lds[wave], g * G, it.L - 1,
+                           lo);
   }
   __syncthreads();
   for (int e = threadIdx.x; e < G * kD; e += kThreads) {

@@ -80,8 +80,9 @@ __device__ __forceinline__ void kv_rows(const QkvArgs& a, int k, int h0, int h1,
       for (int r = 0; r < kRows; ++r)
 #pragma unroll
         for (int p = 0; p < R::kPer; ++p)
-          x[r * R::kPer + p] = load_nt(
-              reinterpret_cast<const uint4*>(src + (size_t)tok[r] * stride) + piece + R::kLanes * p);
+          x[r * R::kPer + p] =
+              load_nt(reinterpret_cast<const uint4*>(src + (size_t)tok[r] * stride) + piece +
+                      R::kLanes * p);
     };
     uint4 ahead[kN];
     load(h0, ahead);
