@@ -7,7 +7,7 @@
 //   a window's masks are made only in steps that a window begins in;
 //   a bias is one multiply-add in the softmax's own slots (fma(dot, scale, bias - reference));
 //   a cap comes before the mask and cannot hide there. Where all of a wavefront's products of a
-//     step are under half the cap it is a polynomial of four multiply-adds a score, else an
+//     step are under half the cap it is a polynomial of five operations a score, else an
 //     exponential, a reciprocal and three more operations.
 // A bias or a cap walks a tile's keys from the last to the first: a steep slope's largest
 // scores then come first, and the softmax's reference moves once instead of at every step.
