@@ -248,3 +248,42 @@ def test_blocks_past_4_gib(cache):
         assert torch.equal(got.view(torch.int16), want.view(torch.int16)) and not got.isnan().any()
         del far, c.kv
         torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("cache", ["bf16", "8bit"])
+def test_chunks_longer_than_their_context(cache):
+    """Rows before a sequence's first token, and sequences without tokens, are zeros; the
+    others as the oracle has them. With nothing asked for, the plain call's bits."""
+    from tests.scored_helpers import Call
+    c = Call([40, 100, 1], [40, 60, 1], hq=8, hkv=2, d=128, cache=cache, seed=11)
+    plain = K.prefill_chunk_fp8 if cache == "8bit" else K.prefill_chunk
+    for lens in ([40, 100, 1], [3, 20, 1], [0, 1, 0], [-5, 59, 1]):
+        say("chunks longer than their context", cache, lens)
+        c.sl.copy_(_i32(lens))
+        c.b.seq_lens = np.maximum(lens, 0).astype(np.int32)
+        want = plain(c.q, c.kv, c.b.num_blocks, c.bt, c.sl, c.cu, num_kv_heads=2,
+                     max_seq_len=112, scale=c.scale)
+        assert torch.equal(c.prefill(max_seq_len=112), want)
+        for kw in (dict(bias=0.0), dict(window=7), dict(softcap=5.0), dict(softcap=5.0, window=7)):
+            c.mods = dict(softcap=kw.get("softcap", 0.0), window=kw.get("window", 0))
+            c.slopes = np.zeros(8, np.float32) if "bias" in kw else None
+            c.dev_slopes = torch.zeros(8, device="cuda") if "bias" in kw else None
+            got = c.prefill(max_seq_len=112)
+            c.check(got, False, f"lens {lens} {kw}")
+            for s, n in enumerate((40, 60, 1)):
+                gone, first = n - max(lens[s], 0), int(c.b.cu_seqlens_q[s])
+                assert gone <= 0 or not got[first:first + gone].any(), (lens, s)
+        c.mods, c.slopes, c.dev_slopes = dict(softcap=0.0, window=0), None, None
+
+
+@pytest.mark.parametrize("cache", ["bf16", "8bit"])
+def test_empty_calls(cache):
+    model = Model(cache, 4)
+    before = model.kv[0].clone()
+    m, table = K.StepMap.empty(0, 0), _i32(np.zeros((0, 4)))
+    q = model.append(0, _rows(0, 0).cuda(), m)
+    assert q.shape == (0, HQ, D)
+    assert model.decode(0, q, table, m, max_seq_len=64).shape == (0, HQ, D)
+    assert model.prefill(0, q, table, m, max_seq_len=64).shape == (0, HQ, D)
+    torch.cuda.synchronize()
+    assert torch.equal(before, model.kv[0])
