@@ -254,3 +254,39 @@ def test_same_bits_in_any_batch():
     assert torch.equal(raw_t(few), raw_t(out[at]))
     written = raw_t(layer) != 0
     assert torch.equal(raw_t(layer)[written], raw_t(big.layer)[written])
+
+
+def _patterns(T, nb, seed):
+    """Slot lists that mix runs in order with single tokens in every way."""
+    r = np.random.default_rng(seed)
+    yield "backwards", np.arange(T)[::-1] + 3
+    a, b = np.arange((T + 1) // 2) + 5, np.arange(T // 2) + 16 * (nb // 2) + 11
+    two = np.empty(T, np.int64)
+    two[0::2], two[1::2] = a, b
+    yield "two sequences by turns", two
+    yield "every other slot", np.arange(T) * 2 + 1
+    runs, free = [], list(r.permutation(nb))
+    while sum(map(len, runs)) < T:           # parts of blocks, 1 to 16 tokens long
+        lo = int(r.integers(0, 16))
+        n = int(r.integers(1, 17 - lo))
+        at = free.pop() * 16 + lo
+        runs.append(np.arange(at, at + n))
+    parts = np.concatenate(runs)[:T]
+    yield "parts of blocks", parts
+    holes = parts.copy()
+    holes[r.random(T) < 0.2] = -1
+    holes[r.random(T) < 0.1] = nb * 16 + 3
+    yield "parts of blocks with holes", holes
+    swapped = parts.copy()
+    i = r.integers(0, T - 1, T // 8)
+    for j in i:
+        swapped[[j, j + 1]] = swapped[[j + 1, j]]
+    yield "parts of blocks, some swapped", swapped
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("T", [17, 33, 130, 515])
+def test_slot_patterns(dtype, d, T):
+    nb = T + 10
+    for what, slots in _patterns(T, nb, T):
+        check(Rows(T, 4, 2, d, dtype, rot=d // 2, nb=nb, slots=slots), what)
