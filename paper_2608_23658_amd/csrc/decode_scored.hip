@@ -7,12 +7,15 @@
 // the window are masked, and their V zeroed, in a wavefront's first step alone. A bias is one
 // multiply-add a score, a cap an exponential and a reciprocal: both disappear behind the loads,
 // which bound a large batch, and cost a small one what its last step's latency grows by. In
-// bf16 and over 8 bits one kernel asks for each score what there is to do. Per call, plain decode / window of 1024 / bias / cap / cap and bias
+// bf16 and over 8 bits one kernel asks what there is to do, once a step for a lane's 16 scores
+// and by scalar branches; asking for each block's four by vector branches, and waiting for the
+// slopes before the first step's loads, cost 0.5 us of one sequence's call (13.7 -> 13.1 with a
+// cap). Per call, plain decode / window of 1024 / bias / cap / cap and bias
 // (32 query heads over 8, head_dim 128, graph replay):
-//   1 sequence of 3971                      11.2 / 13.1 / 13.1 / 13.6 / 14.0 us
-//   12 of 1 to 4096, 64 over 8, d 64        16.5 / 12.2 / 17.8 / 18.5 / 18.8 us
-//   256 of 512 to 4096                       368 /  170 /  369 /  369 /  370 us
-//   6 of 700 to 131071, 8 bits              86.7 / 13.6 / 81.6 / 82.6 / 82.9 us
+//   1 sequence of 3971                      11.3 / 12.7 / 12.6 / 13.1 / 13.4 us
+//   12 of 1 to 4096, 64 over 8, d 64        16.4 / 12.0 / 17.0 / 17.8 / 18.0 us
+//   256 of 512 to 4096                       367 /  169 /  369 /  369 /  369 us
+//   6 of 700 to 131071, 8 bits              86.5 / 13.2 / 81.0 / 82.2 / 82.2 us
 
 #include "decode_split.hpp"
 

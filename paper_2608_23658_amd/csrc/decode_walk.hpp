@@ -145,7 +145,7 @@ __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
   }
 
   float slope = 0.f;
-  if constexpr (Score::kOn) slope = score.slope(h0 + min(head, G - 1));
+  if constexpr (Score::kOn) slope = score.raw_slope(h0 + min(head, G - 1), q);
   float m_run = -INFINITY, l_run = 0.f;   // head's max; the lane's part of its sum
   f32x4_t acc[2 * S::kVI];
 #pragma unroll
@@ -179,7 +179,7 @@ __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
                      const uint4 (&kreg)[S::kTB][S::kVI],
                      uint4 (&vreg)[S::kTB][S::kVI]) __attribute__((always_inline)) {
     // ---- scores ----
-    float x[S::kTB][4];
+    float x[4 * S::kTB];
 #pragma unroll
     for (int j = 0; j < S::kTB; ++j) {
       f32x4_t sc = {0.f, 0.f, 0.f, 0.f};
@@ -188,24 +188,28 @@ __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
         sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kreg[j][i]),
                                                      __builtin_bit_cast(bf16x8_t, qreg[i]), sc, 0,
                                                      0, 0);
-      if constexpr (Score::kOn) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[j][r] = sc[r];
-        score.template cap<false>(x[j]);
-        if (score.slopes) {
-          const float far = (float)(own - (tb + j * S::kBS + row * 4));
-#pragma unroll
-          for (int r = 0; r < 4; ++r) x[j][r] = fmaf(slope, (float)r - far, x[j][r]);
-        }
-      }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int tok = tb + j * S::kBS + row * 4 + r;
         const bool keep = bid[j] >= 0 && (!tail || tok < t1);
         if constexpr (Score::kOn)
-          x[j][r] = keep && tok >= lo ? x[j][r] : -INFINITY;
+          x[4 * j + r] = sc[r];
         else
-          x[j][r] = keep ? sc[r] * score.scale_log2 : -INFINITY;
+          x[4 * j + r] = keep ? sc[r] * score.scale_log2 : -INFINITY;
+      }
+    }
+    if constexpr (Score::kOn) {
+      score.template cap<false>(x);
+      if (score.slopes) {
+        const float by = slope * kLog2e, far = (float)(own - (tb + row * 4));
+#pragma unroll
+        for (int e = 0; e < 4 * S::kTB; ++e)
+          x[e] = fmaf(by, (float)(e / 4 * S::kBS + e % 4) - far, x[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4 * S::kTB; ++e) {
+        const int tok = tb + e / 4 * S::kBS + row * 4 + e % 4;
+        x[e] = bid[e / 4] >= 0 && (!tail || tok < t1) && tok >= lo ? x[e] : -INFINITY;
       }
     }
 
@@ -214,7 +218,7 @@ __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
 #pragma unroll
     for (int j = 0; j < S::kTB; ++j)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[j][r]);
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[4 * j + r]);
     const float mn = cross_row_max(mx);
     const float ref = (mn == -INFINITY) ? 0.f : mn;
     const float alpha = fast_exp2(m_run - ref);
@@ -223,8 +227,8 @@ __device__ __forceinline__ void walk_bf16(const DecodeTiles<kTwo>& tiles,
     uint2 pw[S::kTB];
 #pragma unroll
     for (int j = 0; j < S::kTB; ++j) {
-      pw[j].x = pack_bf16x2(fast_exp2(x[j][0] - ref), fast_exp2(x[j][1] - ref));
-      pw[j].y = pack_bf16x2(fast_exp2(x[j][2] - ref), fast_exp2(x[j][3] - ref));
+      pw[j].x = pack_bf16x2(fast_exp2(x[4 * j] - ref), fast_exp2(x[4 * j + 1] - ref));
+      pw[j].y = pack_bf16x2(fast_exp2(x[4 * j + 2] - ref), fast_exp2(x[4 * j + 3] - ref));
       // the row sum adds the bf16 values that p.v multiplies
       psum = dot2_bf16(pw[j].x, kBf16OnePair, psum);
       psum = dot2_bf16(pw[j].y, kBf16OnePair, psum);

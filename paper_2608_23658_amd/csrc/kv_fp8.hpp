@@ -102,7 +102,7 @@ __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* 
     }
 
   float slope = 0.f;
-  if constexpr (Score::kOn) slope = score.slope(h0 + min(head, G - 1));
+  if constexpr (Score::kOn) slope = score.raw_slope(h0 + min(head, G - 1), q);
   float m_run = -INFINITY, l_run = 0.f;   // head's max; the lane's part of its sum
   f32x4_t acc[4 * kL];
 #pragma unroll
@@ -153,7 +153,7 @@ __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* 
                      const uint4 (&kreg)[kTB][kL],
                      uint4 (&vreg)[kTB][kL]) __attribute__((always_inline)) {
     // ---- scores ----
-    float x[kTB][4];
+    float x[4 * kTB];
 #pragma unroll
     for (int j = 0; j < kTB; ++j) {
       const float ks = fp8_scale(exps[j] & 0xff);
@@ -166,24 +166,28 @@ __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* 
         sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8x8_to_bf16(k.z, k.w, ks, ks), qreg[i][1],
                                                      sc, 0, 0, 0);
       }
-      if constexpr (Score::kOn) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[j][r] = sc[r];
-        score.template cap<false>(x[j]);
-        if (score.slopes) {
-          const float far = (float)(own - (tb + j * kBS + row * 4));
-#pragma unroll
-          for (int r = 0; r < 4; ++r) x[j][r] = fmaf(slope, (float)r - far, x[j][r]);
-        }
-      }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int tok = tb + j * kBS + row * 4 + r;
         const bool keep = bid[j] >= 0 && (!tail || tok < t1);
         if constexpr (Score::kOn)
-          x[j][r] = keep && tok >= lo ? x[j][r] : -INFINITY;
+          x[4 * j + r] = sc[r];
         else
-          x[j][r] = keep ? sc[r] * score.scale_log2 : -INFINITY;
+          x[4 * j + r] = keep ? sc[r] * score.scale_log2 : -INFINITY;
+      }
+    }
+    if constexpr (Score::kOn) {
+      score.template cap<false>(x);
+      if (score.slopes) {
+        const float by = slope * kLog2e, far = (float)(own - (tb + row * 4));
+#pragma unroll
+        for (int e = 0; e < 4 * kTB; ++e)
+          x[e] = fmaf(by, (float)(e / 4 * kBS + e % 4) - far, x[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4 * kTB; ++e) {
+        const int tok = tb + e / 4 * kBS + row * 4 + e % 4;
+        x[e] = bid[e / 4] >= 0 && (!tail || tok < t1) && tok >= lo ? x[e] : -INFINITY;
       }
     }
 
@@ -192,7 +196,7 @@ __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* 
 #pragma unroll
     for (int j = 0; j < kTB; ++j)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[j][r]);
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[4 * j + r]);
     const float mn = cross_row_max(mx);
     const float ref = (mn == -INFINITY) ? 0.f : mn;
     const float alpha = fast_exp2(m_run - ref);
@@ -201,8 +205,8 @@ __device__ __forceinline__ void walk_fp8(const Fp8Tiles& tiles, const uint16_t* 
     uint2 pw[kTB];
 #pragma unroll
     for (int j = 0; j < kTB; ++j) {
-      pw[j].x = pack_bf16x2(fast_exp2(x[j][0] - ref), fast_exp2(x[j][1] - ref));
-      pw[j].y = pack_bf16x2(fast_exp2(x[j][2] - ref), fast_exp2(x[j][3] - ref));
+      pw[j].x = pack_bf16x2(fast_exp2(x[4 * j] - ref), fast_exp2(x[4 * j + 1] - ref));
+      pw[j].y = pack_bf16x2(fast_exp2(x[4 * j + 2] - ref), fast_exp2(x[4 * j + 3] - ref));
       // A weight is rounded to bf16, as the matrix instruction takes it: at most 2^-8 of
       // it, the size of the output's own rounding, and independent from token to
       // token. The row sum adds the rounded weights, so that they still add up to one.

@@ -78,16 +78,23 @@ struct ModScore {
     asm("" : "+v"(s.scale_log2), "+v"(s.cap_log2), "+v"(s.exp_scale));
     return s;
   }
+  // A head's slope, times log2(e) where it is used: a load that nothing waits for here, from
+  // any address that can be read where there is no bias.
+  __device__ __forceinline__ float raw_slope(int head, const void* any) const {
+    return *(slopes ? slopes + head : reinterpret_cast<const float*>(any));
+  }
   // The scores of n products in place. kExact: with the library's tanh.
   template <bool kExact, int n>
   __device__ __forceinline__ void cap(float (&x)[n]) const {
-    if (!has_cap()) {
+    // a wavefront's branches on it are scalar ones
+    const float c = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(cap_log2)));
+    if (!(kForm == Form::kCap || (kForm == Form::kAny && c > 0.f))) {
 #pragma unroll
       for (int e = 0; e < n; ++e) x[e] *= scale_log2;
     } else if constexpr (kExact) {
 #pragma unroll
       for (int e = 0; e < n; ++e) x[e] = cap_log2 * tanhf(x[e] * tanh_scale);
-    } else if (cap_log2 <= kSmallCap) {
+    } else if (c <= kSmallCap) {
 #pragma unroll
       for (int e = 0; e < n; ++e) x[e] = capped_far(x[e], exp_scale, cap_log2);
     } else {
