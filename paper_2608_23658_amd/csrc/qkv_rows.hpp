@@ -249,7 +249,8 @@ __device__ __forceinline__ void q_rows(const QkvArgs& a, int wg, int groups, int
 // How rows are dealt to wavefronts: more heads to each where there are enough to fill the
 // card anyway. 8192 / 2048 tokens, 32 query heads over 8: at these bounds 43.5 / 19.2 us, at half
 // of them 43.5 / 18.5 (but 1777 tokens of 12 over 3 in fp32 8.2 instead of 7.4), at twice
-// 42.0 / 20.9 (4096 tokens of 64 over 8, 8 bits, 39.2 instead of 36.4).
+// 42.0 / 20.9 (4096 tokens of 64 over 8, 8 bits, 39.2 instead of 36.4). Then as many to each of a
+// workgroup's wavefronts (46 heads over 1: 46.2 -> 42.0 us).
 struct QkvSplit {
   int per_wave, groups;   // heads of a wavefront, workgroups of a run
   long long workgroups;
@@ -258,6 +259,7 @@ inline QkvSplit qkv_split(long long runs, int heads) {
   QkvSplit s;
   s.per_wave = runs * heads > 8192 ? 8 : runs * heads > 4096 ? 4 : runs * heads > 2048 ? 2 : 1;
   s.groups = (heads + kQkvWaves * s.per_wave - 1) / (kQkvWaves * s.per_wave);
+  s.per_wave = (heads + kQkvWaves * s.groups - 1) / (kQkvWaves * s.groups);   // in even parts
   s.workgroups = runs * s.groups;
   return s;
 }
