@@ -221,10 +221,9 @@ __device__ __forceinline__ PlanTotals plan_totals(PlanTotals v, PlanTotals* lds)
 }
 
 // Tile t of a chunk of sequences: its sequence's index in the chunk, first row,
-// key steps, from i0 (what its first row's window leaves out) to i1.
+// key steps.
 struct PlanTile {
-  int idx, q0, i0, i1;
-  __device__ __forceinline__ int steps() const { return i1 - i0; }
+  int idx, q0, steps;
 };
 
 struct PlanChoice {
@@ -296,13 +295,12 @@ __global__ __launch_bounds__(kPlanThreads) void prefill_plan_kernel(PlanArgs arg
     const int n = seq_n[lo], L = seq_L[lo];
     r.idx = lo;
     r.q0 = (nt - 1 - (t - first[lo])) * R;
-    const int last_pos = min(L - n + r.q0 + min(R, n - r.q0) - 1, L - 1);
-    r.i1 = last_pos >= 0 ? last_pos / kKeys + 1 : 0;
-    r.i0 = min(first_step(L - n + r.q0, a.window), r.i1);
+    const int pos = L - n + r.q0;
+    r.steps = walk_steps(pos, min(pos + min(R, n - r.q0) - 1, L - 1), a.window);
     return r;
   };
   // First token of a one-row sequence's item, and how many there are from it on.
-  auto row_from = [&](int L) { return max(0, L - a.window) / kKeys * kKeys; };
+  auto row_from = [&](int L) { return walk_start(L - 1, a.window); };
 
   if (tid == 0) {
     extra_row_items = 0;
@@ -321,12 +319,12 @@ __global__ __launch_bounds__(kPlanThreads) void prefill_plan_kernel(PlanArgs arg
   const int lanes = max(1, kNumCUs / a.num_kv_heads);
   int chunk_tiles = kResident ? min(found.total, kPlanThreads) : found.total;
   int all_tiles = chunk_tiles, all_rows = found.set_total;
-  PlanTile own = {0, 0, 0, 0};
+  PlanTile own = {0, 0, 0};
   // Whole tiles and one-row sequences that all run at once, in any order.
   const bool one_round = kResident && chunk_tiles + all_rows <= min(lanes, a.max_items);
   auto write_whole = [&] {
     if (tid < chunk_tiles)
-      a.items[tid] = {own.idx, own.q0, own.i0, own.i1, -1, seq_cu[own.idx], seq_n[own.idx],
+      a.items[tid] = {own.idx, own.q0, 0, own.steps, -1, seq_cu[own.idx], seq_n[own.idx],
                       seq_L[own.idx]};
     if (a.rows && tid < a.num_seqs && seq_n[tid] == 1)
       a.items[chunk_tiles + found.set_before] = {tid, -1, row_from(seq_L[tid]), seq_L[tid], -1,
@@ -335,7 +333,7 @@ __global__ __launch_bounds__(kPlanThreads) void prefill_plan_kernel(PlanArgs arg
   };
   if constexpr (kResident) {
     if (tid < chunk_tiles) own = tile_of(tid);
-    steps[tid] = own.steps();
+    steps[tid] = own.steps;
     if (one_round && a.max_slots == 0 && a.max_row_slots == 0) {
       write_whole();
       return;
@@ -366,8 +364,8 @@ __global__ __launch_bounds__(kPlanThreads) void prefill_plan_kernel(PlanArgs arg
   PlanTotals sum = {0.f, 0.f, 1.f, 1.f};
   each(
       [&](int, const PlanTile& t) {
-        sum.steps += t.steps();
-        sum.max_steps = fmaxf(sum.max_steps, t.steps());
+        sum.steps += t.steps;
+        sum.max_steps = fmaxf(sum.max_steps, t.steps);
       },
       [&](int, int, int L) {
         const int tokens = L - row_from(L);
@@ -483,7 +481,7 @@ __global__ __launch_bounds__(kPlanThreads) void prefill_plan_kernel(PlanArgs arg
   auto row_bucket = [&](int per) { return 255 - min(255, (int)(per * row_per_bucket)); };
   each(
       [&](int, const PlanTile& t) {
-        const int2 p = tile_pieces(t.steps(), C);
+        const int2 p = tile_pieces(t.steps, C);
         atomicAdd(&hist[bucket(p.x)], p.y);
       },
       [&](int, int, int L) {
@@ -519,7 +517,7 @@ __global__ __launch_bounds__(kPlanThreads) void prefill_plan_kernel(PlanArgs arg
   };
   each(
       [&](int base, const PlanTile& t) {
-        const int2 p = tile_pieces(t.steps(), C);
+        const int2 p = tile_pieces(t.steps, C);
         const int j0 = atomicAdd(&hist[bucket(p.x)], p.y);
         const int cu0 = seq_cu[t.idx], n = seq_n[t.idx], L = seq_L[t.idx];
         int slot = -1;
@@ -531,7 +529,7 @@ __global__ __launch_bounds__(kPlanThreads) void prefill_plan_kernel(PlanArgs arg
         for (int k = 0; k < p.y; ++k) {
           const int pos = tile_pos(j0 + k);
           if (pos < a.max_items)
-            a.items[pos] = {base + t.idx, t.q0, t.i0 + k * p.x, min(t.i1, t.i0 + (k + 1) * p.x),
+            a.items[pos] = {base + t.idx, t.q0, k * p.x, min(t.steps, (k + 1) * p.x),
                             slot < 0 ? -1 : slot + k, cu0, n, L};
         }
       },
@@ -760,10 +758,10 @@ static hipError_t launch_prefill_t(const PrefillArgs& a) {
   // sequences or tiles shares none.
   const long long bound = (long long)a.total_q_tokens / kRowsPerTile + a.num_seqs;
   const bool resident = a.num_seqs <= kPlanThreads && bound <= kPlanThreads;
-  // what a tile (from an even step on) and a one-row sequence walk at most
+  // what a tile and a one-row sequence walk at most
   const int window = a.mods ? window_keys(*a.mods) : kNoWindow;
-  const int most_keys = std::min(a.max_seq_len, window + kRowsPerTile + 2 * kKeys);
-  const int most_row = std::min(a.max_seq_len, window + kKeys);
+  const int most_keys = std::min(a.max_seq_len, window + kRowsPerTile + kBS);
+  const int most_row = std::min(a.max_seq_len, window + kBS);
   const long long steps = ((long long)most_keys + kKeys - 1) / kKeys;
   const long long tile_wgs = (long long)(a.total_q_tokens / kRowsPerTile) * a.num_kv_heads;
   const bool share = resident && sharing_pays(steps, tile_wgs, kLaunchSteps);

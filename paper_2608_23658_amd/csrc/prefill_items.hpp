@@ -3,6 +3,7 @@
 #pragma once
 
 #include "common.hpp"
+#include "window.hpp"
 
 namespace kvattn {
 
@@ -17,6 +18,7 @@ constexpr float kPsumBound = 256.f;         // 2^kLazyRescale
 constexpr int kWaves = 8;                  // wavefronts per workgroup
 constexpr int kThreads = kWaves * kWave;
 constexpr int kNumCUs = 256;               // gfx950
+static_assert(kBS == 16 && kKeys == 64, "as window.hpp takes them");
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
@@ -109,16 +111,11 @@ __device__ __forceinline__ int2 chunk_rows(const int* __restrict__ cu, int s, in
 
 struct PrefillItem {
   int s, q0;        // sequence, first row of the tile in the chunk (-1: one-row item)
-  int i0, i1;       // key steps, i0 even (one-row item: tokens, i0 a multiple of 64)
+  int i0, i1;       // key steps from the tile's walk_start on, i0 even (one-row item: tokens,
+                    // i0 a multiple of 16)
   int slot;         // partial slot, -1: written to out
   int cu0, n, L;    // the sequence's chunk and clamped length
 };
-
-// First key step, an even one, of a tile whose first row is at position pos, where a
-// row sees window keys.
-__device__ __forceinline__ int first_step(int pos, int window) {
-  return max(0, pos - window + 1) / kKeys & ~1;
-}
 
 // The item of workgroup (ti, kv head) of a launch without a plan: tile ti of the tile map.
 __device__ __forceinline__ PrefillItem whole_tile(const int2* __restrict__ tiles, int ti,
@@ -133,9 +130,9 @@ __device__ __forceinline__ PrefillItem whole_tile(const int2* __restrict__ tiles
   it.cu0 = rows.x;
   it.n = rows.y - rows.x;
   it.L = min(max(seq_lens[tl.x], 0), max_tokens);
-  const int last_pos = min(it.L - it.n + it.q0 + min(rows_per_tile, it.n - it.q0) - 1, it.L - 1);
-  it.i1 = last_pos >= 0 ? last_pos / kKeys + 1 : 0;
-  it.i0 = min(first_step(it.L - it.n + it.q0, window), it.i1);
+  const int pos = it.L - it.n + it.q0;
+  it.i0 = 0;
+  it.i1 = walk_steps(pos, min(pos + min(rows_per_tile, it.n - it.q0) - 1, it.L - 1), window);
   it.slot = -1;
   return it;
 }

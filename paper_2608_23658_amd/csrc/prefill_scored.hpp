@@ -1,8 +1,8 @@
 // Chunked prefill with scores that are capped, biased by distance or cut to a window: the
 // tile pipeline of prefill_tile.hpp, with scores made by ModScore.
 //
-// The plan cuts a tile's key steps to those that its rows' windows reach (an even first step, as
-// the pipeline takes steps by twos) and prices items by what is left. The matrix
+// A tile's steps begin with the block of the first key that its first row sees (window.hpp), so
+// that nothing before it is read, and the plan prices items by what is left. The matrix
 // work of a step takes a little longer than its softmax beside it, so what a score costs more shows:
 //   a window's masks are made only in steps that a window begins in;
 //   a bias is one multiply-add in the softmax's own slots (fma(dot, scale, bias - reference));

@@ -60,7 +60,7 @@ constexpr int kVBufs = 3;                  // LDS V steps (gathered one step ahe
 struct TileEnd {
   uint16_t* out;    // of this kv head's first query head, row 0
   uint8_t* slots;   // of this kv head, slot 0
-  int slot, cu0, n, qstride, num_kv_heads;
+  int slot, cu0, n, qstride, num_kv_heads, q0;
 };
 
 // One item of a work tile. With ModScore a row sees the keys of its window alone; what slots
@@ -76,8 +76,18 @@ __device__ __forceinline__ void prefill_tile(
   const int lane = tid % kWave;
   const int h = g * G + wave % G;
   const int s = it.s, q0 = it.q0, cu0 = it.cu0, n = it.n;
-  const int L = __builtin_amdgcn_readfirstlane(it.L);
   const int row0 = q0 + (wave / G) * 32;        // first row of this wave
+  // With ModScore keys, table entries and steps count from the block of the first key that any
+  // row of the tile sees on (walk_start); lo: that key.
+  int L = __builtin_amdgcn_readfirstlane(it.L), lo = 0;
+  const int* bt = block_table + (size_t)s * max_blocks;
+  if constexpr (Score::kOn) {
+    lo = score.first_key(L - n + q0);
+    const int start = __builtin_amdgcn_readfirstlane(walk_start(L - n + q0, score.window));
+    bt += start / kBS;
+    lo -= start;
+    L -= start;
+  }
   const int c = L - n;                          // cached context before the chunk
   const int i0 = it.i0, N = it.i1;              // steps of the item
   __builtin_assume(i0 >= 0 && N >= 0);
@@ -89,15 +99,12 @@ __device__ __forceinline__ void prefill_tile(
     return Score::form == Form::kBias || Score::form == Form::kCap ? ends - i : i;
   };
   const bool idle = row0 >= n;                  // none of the wave's 32 rows is in the chunk
-  // first key that any row of the tile sees
-  int lo = 0;
-  if constexpr (Score::kOn) lo = score.first_key(c + q0);
   // With ModScore the loop has no scalar registers to spare: kept in LDS until the end.
   __shared__ TileEnd lds_end;
   if constexpr (Score::kOn)
     if (tid == 0)
       lds_end = {out + (size_t)g * G * kD, slots + (size_t)g * kSlotBytes, it.slot, cu0, n,
-                 num_q_heads * kD, num_kv_heads};
+                 num_q_heads * kD, num_kv_heads, q0};
   float slope = 0.f;
   __shared__ float lds_slope[kWaves];   // with a cap, which leaves no register for it
   if constexpr (Score::kOn) {
@@ -116,7 +123,6 @@ __device__ __forceinline__ void prefill_tile(
   const int block_shift = kPow2Blocks ? __builtin_ctzll((size_t)block_bytes) : 0;
   const Off k_off = (Off)g * kTileBytes;
   const Off v_off = (Off)(num_kv_heads + g) * kTileBytes;
-  const int* bt = block_table + (size_t)s * max_blocks;
   const int qstride = num_q_heads * kD;
 
   const int lm = lane % 32;     // MFMA row / column index of this lane
@@ -595,16 +601,18 @@ __device__ __forceinline__ void prefill_tile(
   // ---- write O (this lane: row lm): normalised, or the item's partial ----
   {
     TileEnd end;
+    int w = wave;
     if constexpr (Score::kOn) {
       int first = i0;
-      asm volatile("" : "+s"(first));   // as above
+      asm volatile("" : "+s"(first), "+s"(w));   // as above
       if (N <= first) __syncthreads();  // no step has published lds_end
       end = lds_end;
       end.slot = __builtin_amdgcn_readfirstlane(end.slot);
     } else {
       end = {out + (size_t)g * G * kD, slots + (size_t)g * kSlotBytes, it.slot, cu0, n, qstride,
-             num_kv_heads};
+             num_kv_heads, q0};
     }
+    const int row0 = end.q0 + (w / G) * 32;
     const float lt = l_run + __shfl_xor(l_run, 32, kWave);
     const int r = row0 + lm;
     if (end.slot < 0) {

@@ -56,8 +56,18 @@ __device__ __forceinline__ void prefill_tile_fp8(
   const int lane = tid % kWave;
   const int h = g * G + wave % G;
   const int s = it.s, q0 = it.q0, cu0 = it.cu0, n = it.n;
-  const int L = __builtin_amdgcn_readfirstlane(it.L);
   const int row0 = q0 + (wave / G) * 32;        // first row of this wave
+  // With ModScore keys, table entries and steps count from the block of the first key that any
+  // row of the tile sees on (walk_start); lo: that key.
+  int L = __builtin_amdgcn_readfirstlane(it.L), lo = 0;
+  const int* bt = block_table + (size_t)s * max_blocks;
+  if constexpr (Score::kOn) {
+    lo = score.first_key(L - n + q0);
+    const int start = __builtin_amdgcn_readfirstlane(walk_start(L - n + q0, score.window));
+    bt += start / kBS;
+    lo -= start;
+    L -= start;
+  }
   const int c = L - n;                          // cached context before the chunk
   const int i0 = it.i0, N = it.i1;              // steps of the item
   __builtin_assume(i0 >= 0 && N >= 0);
@@ -69,9 +79,6 @@ __device__ __forceinline__ void prefill_tile_fp8(
     return Score::form == Form::kBias || Score::form == Form::kCap ? ends - i : i;
   };
   const bool idle = row0 >= n;                  // none of the wave's 32 rows is in the chunk
-  // first key that any row of the tile sees
-  int lo = 0;
-  if constexpr (Score::kOn) lo = score.first_key(c + q0);
   float slope = 0.f;
   __shared__ float lds_slope[kWaves];   // with a cap, which leaves no register for it
   if constexpr (Score::kOn) {
@@ -95,7 +102,6 @@ __device__ __forceinline__ void prefill_tile_fp8(
                num_q_heads * kD, num_kv_heads};
 
   const Fp8Tiles tiles(kv, num_kv_heads, kD, g);
-  const int* bt = block_table + (size_t)s * max_blocks;
   const int qstride = num_q_heads * kD;
 
   const int lm = lane % 32;     // MFMA row / column index of this lane

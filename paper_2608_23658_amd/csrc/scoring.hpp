@@ -6,10 +6,9 @@
 
 #include "common.hpp"
 #include "launch.hpp"
+#include "window.hpp"
 
 namespace kvattn {
-
-constexpr int kNoWindow = 0x3fffffff;
 
 // What the scores of a kernel can be; all but plain ones have a window. kAny asks for each
 // score.
@@ -52,7 +51,9 @@ struct ModScore {
     return slopes ? slopes[head] * kLog2e : 0.f;
   }
   // First key that the row at position pos sees.
-  __device__ __forceinline__ int first_key(int pos) const { return max(0, pos - window + 1); }
+  __device__ __forceinline__ int first_key(int pos) const {
+    return kvattn::first_key(pos, window);
+  }
 
   // cap tanh(dot scale / cap) as cap (1 - 2 / (e^2x + 1)), off by 2^-22 of the cap, which for
   // one up to kSmallCap is 2^-14 of a weight; for a larger one, near zero, by kTanh4. kExact:

@@ -188,3 +188,26 @@ def test_streams_and_graphs():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(want, kw["out"]), turn
+
+
+@pytest.mark.parametrize("cache", CACHES)
+@pytest.mark.parametrize("mods", [dict(), dict(softcap=20.0), dict(bias=True)])
+@pytest.mark.parametrize("window", [20, 90, 1000])
+def test_ids_behind_a_window_may_be_others(cache, mods, window):
+    """Entries of blocks before the first row's window still name blocks of the layer, which
+    others have by now and which hold anything: NaN here, in every slot and exponent."""
+    say("prefill stale ids", cache, mods, window)
+    lens, new = [window + 31, 1700, 2048, 1111, 1500], [30, 1, 200, 64, 1]
+    c = Call(lens, new, hq=8, hkv=2, d=128, cache=cache, window=window, **mods)
+    small = _small(c)
+    want, whole = c.prefill(), c.prefill(ws=small)
+    c.check(want, False, f"{cache} window {window} {mods}")
+    c.check(whole, False, f"{cache} window {window} {mods}, whole tiles")
+    given_up = []
+    for s, (L, n) in enumerate(zip(lens, new)):
+        given_up += list(c.b.block_table[s][:max(0, L - n - window + 1) // 16])
+    layer = c.kv.clone().view(c.b.num_blocks, -1)
+    layer[torch.tensor(sorted(given_up)).cuda()] = 0xff if cache == "8bit" else float("nan")
+    c.kv = layer.view(c.kv.shape)
+    assert torch.equal(want.view(torch.int16), c.prefill().view(torch.int16))
+    assert torch.equal(whole.view(torch.int16), c.prefill(ws=small).view(torch.int16))
