@@ -15,9 +15,10 @@
 //   q along the lanes with loads ahead, K and V by blocks, V through LDS           57.2
 //   K along the lanes and heads one after another with loads ahead too             51.5
 //   both dims of a pair in a lane (LaneRows::kPairsIn)                             43.5
-// (32 query heads over 8; 16 over 16 83.4 -> 43.2). 256 scattered tokens: 15.1 us, or 10.3 in a
-// graph with the inputs in the caches. There each of V's 2-byte elements goes into a 32-byte
-// run of its own, a quarter of a million of them.
+//   no private memory, addresses made where they are used (kv_rows)                39.9
+// (32 query heads over 8; 16 over 16 83.4 -> 38.9). 256 scattered tokens: 14.5 us, of inputs not
+// in a cache. There each of V's 2-byte elements goes into a 32-byte run of its own, a quarter of
+// a million of them.
 //
 // A run of K or V is the tokens of one block where tokens follow each other in slot order, so
 // that a block is written whole by one wavefront wherever a chunk begins in it; tokens
@@ -41,6 +42,10 @@ __device__ __forceinline__ void kv_rows(const QkvArgs& a, int k, int h0, int h1,
   const int lane = threadIdx.x % kWave;
   const int hkv = a.num_kv_heads;
   constexpr size_t kTile = (size_t)kRunTokens * D * ESZ;
+  // Values before one is chosen: a choice among a's members became one of their addresses, which
+  // kept a in private memory, 40 bytes a lane that every wavefront wrote and read back.
+  const uint8_t *k_rows = a.k, *v_rows = a.v;
+  const size_t k_stride = a.k_stride, v_stride = a.v_stride;
 
   // Lane l looks at token 16 (k - 1) + l; the run's are among lanes 1 .. 31.
   const int t = kRunTokens * (k - 1) + lane;
@@ -73,16 +78,21 @@ __device__ __forceinline__ void kv_rows(const QkvArgs& a, int k, int h0, int h1,
       tok[r] = kRunTokens * (k - 1) + __shfl(packed, i16, kWave);
     }
     auto load = [&](int h, uint4 (&x)[kN]) __attribute__((always_inline)) {
-      const uint8_t* src =
-          h < hkv ? a.k + (size_t)h * (D * ESZ) : a.v + (size_t)(h - hkv) * (D * ESZ);
-      const size_t stride = h < hkv ? a.k_stride : a.v_stride;
+      const uint8_t* src = (h < hkv ? k_rows : v_rows) + (size_t)(h < hkv ? h : h - hkv) * (D * ESZ);
+      const size_t stride = h < hkv ? k_stride : v_stride;
+      // addresses are made here: kept over the heads, one for each stride, they took the third
+      // wavefront of a SIMD (178 registers instead of 168)
+      int at = piece;
+      asm volatile("" : "+v"(at));
 #pragma unroll
-      for (int r = 0; r < kRows; ++r)
+      for (int r = 0; r < kRows; ++r) {
+        int t = tok[r];
+        asm volatile("" : "+v"(t));
 #pragma unroll
         for (int p = 0; p < R::kPer; ++p)
           x[r * R::kPer + p] =
-              load_nt(reinterpret_cast<const uint4*>(src + (size_t)tok[r] * stride) + piece +
-                      R::kLanes * p);
+              load_nt(reinterpret_cast<const uint4*>(src + (size_t)t * stride) + at + R::kLanes * p);
+      }
     };
     uint4 ahead[kN];
     load(h0, ahead);

@@ -32,3 +32,16 @@ def test_m0_is_saved_and_restored(disassembly):  # noqa: F811
             saved = ins[a - 3][1].split(",")[0]
             assert ins[a - 3] == ("s_mov_b32", f"{saved},m0"), (name, ins[a - 3])
             assert ins[b + 1] == ("s_mov_b32", f"m0,{saved}"), (name, ins[b + 1])
+
+
+def test_no_kernel_has_private_memory(disassembly):  # noqa: F811
+    """No call allocates: a kernel with private memory has the runtime set up scratch for the
+    queue on its first launch, and each of its wavefronts writes and reads it."""
+    notes = disassembly[1]
+    names = re.findall(r"\.symbol:\s+(\S+)", notes)
+    private = [int(x) for x in re.findall(r"\.private_segment_fixed_size:\s+(\d+)", notes)]
+    assert len(names) == len(private) >= 300, (len(names), len(private))
+    assert sum("qkv_append_kernel" in n for n in names) == 24
+    assert not re.findall(r"\.uses_dynamic_stack:\s+true", notes)
+    bad = [(n, b) for n, b in zip(names, private) if b]
+    assert not bad, bad
