@@ -326,9 +326,9 @@ typedef struct {
  * scale * log2(e) must be finite. With a window, what is read of a sequence is the last
  * window tokens: table entries of blocks wholly before them are not read, and what the
  * window's first block holds before its first token has no effect, NaN included. A workspace
- * for min(max_seq_len, window + 15) tokens is enough. A capped score is off by at
- * most softcap * 2^-21 (in fp32, by what the library's tanh is). A sequence's bits depend on
- * itself, scoring and scale alone.
+ * for min(max_seq_len, window + 15) tokens is enough. A capped score is off by at most
+ * softcap * 2^-21, and past a softcap of 177 by at most 2^-19 of itself (in fp32, by what the
+ * library's tanh is). A sequence's bits depend on itself, scoring and scale alone.
  * Supported: as kvattn_decode (bf16 with head_dim 64 or 128, fp32 with 64) and
  * kvattn_decode_fp8. */
 int kvattn_decode_scored(const void* q, const void* kv_layer, int num_blocks,
@@ -349,9 +349,10 @@ int kvattn_decode_scored_fp8(const void* q, const void* kv_layer, int num_blocks
  * workspaces and rules but that scale may have any sign (scale * log2(e) finite). With a
  * window, table entries of blocks wholly before the window of a chunk's first row are not
  * used for anything, and what lies before it in that window's first block has no effect,
- * NaN included. A row that sees no key (its ids outside the layer) gets zeros. Rows behind
- * cu_seqlens_q[num_seqs] are left as they are. What a row's bits depend on is as said there,
- * but that what a window leaves out of a tile or sequence does not count for its length.
+ * NaN included. A capped score is off by as much as in decode. A row that sees no key (its
+ * ids outside the layer) gets zeros. Rows behind cu_seqlens_q[num_seqs] are left as they are.
+ * What a row's bits depend on is as said there, but that what a window leaves out of a tile
+ * or sequence does not count for its length.
  * Supported: as those (head_dim 128). */
 int kvattn_prefill_chunk_scored(const void* q, const void* kv_layer, int num_blocks,
                                 const int32_t* block_table, const int32_t* seq_lens,

@@ -601,10 +601,10 @@ __device__ __forceinline__ void prefill_tile(
   // ---- write O (this lane: row lm): normalised, or the item's partial ----
   {
     TileEnd end;
-    int w = wave;
+    int wv = wave;
     if constexpr (Score::kOn) {
       int first = i0;
-      asm volatile("" : "+s"(first), "+s"(w));   // as above
+      asm volatile("" : "+s"(first), "+s"(wv));   // as above
       if (N <= first) __syncthreads();  // no step has published lds_end
       end = lds_end;
       end.slot = __builtin_amdgcn_readfirstlane(end.slot);
@@ -612,7 +612,7 @@ __device__ __forceinline__ void prefill_tile(
       end = {out + (size_t)g * G * kD, slots + (size_t)g * kSlotBytes, it.slot, cu0, n, qstride,
              num_kv_heads, q0};
     }
-    const int row0 = end.q0 + (w / G) * 32;
+    const int row0 = end.q0 + (wv / G) * 32;
     const float lt = l_run + __shfl_xor(l_run, 32, kWave);
     const int r = row0 + lm;
     if (end.slot < 0) {
@@ -625,7 +625,7 @@ __device__ __forceinline__ void prefill_tile(
       // 10.6 us; tiles of hundreds of steps do not notice.
       constexpr int kHalf = kD / 2, kRowBytes = kHalf * 2 + 16;   // padded against conflicts
       static_assert(kWaves * 32 * kRowBytes <= (int)sizeof(lds_k), "fits the K buffers");
-      uint8_t* stage = &lds_k[0][0][0] + wave * 32 * kRowBytes;
+      uint8_t* stage = &lds_k[0][0][0] + wv * 32 * kRowBytes;
       const float inv = lt > 0.f ? 1.f / lt : 0.f;
       const int sr = lane / 16, sc = lane % 16;   // row of four, 8-byte piece of its half
 #pragma unroll
@@ -646,18 +646,18 @@ __device__ __forceinline__ void prefill_tile(
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int rr = 4 * j + sr;
-          const uint2 w = *reinterpret_cast<const uint2*>(stage + rr * kRowBytes + sc * 8);
+          const uint2 x = *reinterpret_cast<const uint2*>(stage + rr * kRowBytes + sc * 8);
           if (row0 + rr < end.n)
             *reinterpret_cast<uint2*>(end.out +
                                       (size_t)(end.cu0 + row0 + rr) * end.qstride +
-                                      (wave % G) * kD + half * kHalf + sc * 4) = w;
+                                      (wv % G) * kD + half * kHalf + sc * 4) = x;
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
       }
     } else if (r < end.n) {
       uint8_t* slot = end.slots + (size_t)end.slot * end.num_kv_heads * kSlotBytes;
-      float2* po = reinterpret_cast<float2*>(slot) + wave * 32 * (kD / 2) + lm;
+      float2* po = reinterpret_cast<float2*>(slot) + wv * 32 * (kD / 2) + lm;
 #pragma unroll
       for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -665,7 +665,7 @@ __device__ __forceinline__ void prefill_tile(
           po[(dt * 16 + (a / 2) * 4 + lh * 2 + a % 2) * 32] =
               make_float2(oacc[dt][2 * a], oacc[dt][2 * a + 1]);
       if (lh == 0)
-        reinterpret_cast<float2*>(slot + kSlotFloats * sizeof(float))[wave * 32 + lm] =
+        reinterpret_cast<float2*>(slot + kSlotFloats * sizeof(float))[wv * 32 + lm] =
             make_float2(m_ref, lt);
     }
   }

@@ -28,6 +28,9 @@ struct PlainScore {
 constexpr float kTanh4[4] = {-0.333326216f, 0.133135208f, -0.0522311078f, 0.0156404821f};
 constexpr float kTanh3[3] = {-0.333282646f, 0.132067148f, -0.0447894702f};
 
+// kTanh3 in y = 2 log2(e) z.
+constexpr float kTanhY[3] = {-0.0400316641f, 0.00190535828f, -7.76155430e-05f};
+
 // a = scale q.k; a = cap tanh(a / cap); a += slope (key - row); keys from row - window + 1 on.
 // All in the log2 domain.
 template <Form kForm>
@@ -69,6 +72,17 @@ struct ModScore {
     h = fmaf(h, w, kTanh4[1]);
     h = fmaf(h, w, kTanh4[0]);
     return z * cap_log2 * fmaf(h, w, 1.f);
+  }
+
+  // The one or the other by the product's size, where a cap is large: off by 2^-19 of the
+  // score. In y = 2 log2(e) z, which the exponential takes, so that a prefill tile needs no
+  // register more.
+  static __device__ __forceinline__ float capped_each(float dot, float exp_scale, float cap_log2,
+                                                      float scale_log2) {
+    const float y = dot * exp_scale, w = y * y;
+    const float h = fmaf(fmaf(w, kTanhY[2], kTanhY[1]), w, kTanhY[0]);
+    const float far = fmaf(-2.f * cap_log2, __builtin_amdgcn_rcpf(fast_exp2(y) + 1.f), cap_log2);
+    return fabsf(y) < kLog2e ? dot * scale_log2 * fmaf(h, w, 1.f) : far;
   }
 
   // ---- for a walk, some scores at a time ----
@@ -147,12 +161,21 @@ struct ModScore {
           const float x = s[e / 16][e % 16], t = x * x;
           s[e / 16][e % 16] = x * fmaf(fmaf(fmaf(t, c3, c2), t, c1), t, c0);
         }
-      } else {
+      } else if (small_cap()) {
         float scale = exp_scale, cap = cap_log2;
         here(scale, cap);
 #pragma unroll
         for (int e = 0; e < 32; ++e)
           s[e / 16][e % 16] = capped_far(s[e / 16][e % 16], scale, cap);
+      } else {
+        // each by its own size: one large product must not cost the others' scores
+        float scale = exp_scale, cap = cap_log2, near = p0;
+        here(scale, cap, near);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          s[e / 16][e % 16] = capped_each(s[e / 16][e % 16], scale, cap, near);
+          __builtin_amdgcn_sched_barrier(0);   // no registers for more at a time
+        }
       }
       const float slope =
           __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(slope_log2)));
@@ -173,6 +196,12 @@ struct ModScore {
       for (int e = 0; e < 32; ++e) s[e / 16][e % 16] *= scale_log2;
       return {1.f, slope_log2, first};
     }
+  }
+  // cap_log2 <= kSmallCap, compared by its bits each time: no mask is kept.
+  __device__ __forceinline__ bool small_cap() const {
+    uint32_t c = __float_as_uint(cap_log2);
+    asm volatile("" : "+s"(c));
+    return c <= __float_as_uint(kSmallCap);
   }
   // Whether all of a wavefront's products are smaller than near.
   template <typename V>

@@ -3,9 +3,10 @@ import numpy as np
 import pytest
 import torch
 
+import oracle
 import paper_2608_23658_amd.kvattn as K
-from tests.gpu_helpers import require_gpu, say
-from tests.scored_helpers import MODS, Call
+from tests.gpu_helpers import f64, require_gpu, say
+from tests.scored_helpers import MODS, Call, assert_scored
 from tests.test_gpu_scored_decode import _poison
 
 pytestmark = pytest.mark.gpu
@@ -211,3 +212,28 @@ def test_ids_behind_a_window_may_be_others(cache, mods, window):
     c.kv = layer.view(c.kv.shape)
     assert torch.equal(want.view(torch.int16), c.prefill().view(torch.int16))
     assert torch.equal(whole.view(torch.int16), c.prefill(ws=small).view(torch.int16))
+
+
+@pytest.mark.parametrize("cache", CACHES)
+@pytest.mark.parametrize("softcap", [1e4, 1e5, 1e6])
+def test_a_large_product_beside_small_ones_under_a_large_cap(cache, softcap):
+    """One row's products pass half the cap, the others' scores are of a few units: theirs are
+    as exact as under a small cap (off by at most 2^-19 of themselves)."""
+    say("prefill large cap", cache, softcap)
+    for lens, new, big in (([40], [33], 5), ([700, 90], [200, 40], 150)):
+        c = Call(lens, new, hq=4, hkv=2, d=128, cache=cache, softcap=softcap, seed=11)
+        # every head of one row: a query along a key that it sees, of 0.8 caps
+        k, _ = oracle.gather_kv(c.b.kv_raw(), c.b.dtype, c.b.block_table[0], lens[0], 2, 16, 128)
+        at = lens[0] - new[0] + big
+        for h in range(4):
+            key = torch.from_numpy(k[at - 3, h // 2]).float()
+            row = key * (0.8 * softcap / (float(key @ key) * c.scale))
+            c.b.q[big, h] = row.to(c.b.q.dtype)
+        c.q = c.b.q.cuda()
+        got = f64(c.prefill())
+        ref, weight = c.expected(False)
+        others = np.arange(sum(new)) != big
+        what = f"{cache} cap {softcap} of {lens}"
+        assert_scored(got[others], ref[others], weight[others], cache, 0.0, what)
+        # its own: 2^-19 of scores up to the cap; the key it points at is most of the sum
+        assert_scored(got[big], ref[big], weight[big], cache, 4 * softcap, what + ", its row")
