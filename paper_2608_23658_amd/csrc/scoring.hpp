@@ -236,8 +236,8 @@ ModScore<kForm> mod_score(float scale, const ScoreMods& m) {
   s.p1 = s.p0 * w * kTanh3[0];
   s.p2 = s.p0 * w * w * kTanh3[1];
   s.p3 = s.p0 * w * w * w * kTanh3[2];
-  // none is near where a coefficient has left fp32's range (a tiny cap)
-  s.near = w < 1e9f && std::isfinite(s.p3) ? 0.5f / std::fabs(s.tanh_scale) : 0.f;
+  // none is near where a coefficient has left fp32's normal range (a tiny cap, a tiny scale)
+  s.near = w < 1e9f && std::isnormal(s.p3) ? 0.5f / std::fabs(s.tanh_scale) : 0.f;
   return s;
 }
 

@@ -237,3 +237,16 @@ def test_a_large_product_beside_small_ones_under_a_large_cap(cache, softcap):
         assert_scored(got[others], ref[others], weight[others], cache, 0.0, what)
         # its own: 2^-19 of scores up to the cap; the key it points at is most of the sum
         assert_scored(got[big], ref[big], weight[big], cache, 4 * softcap, what + ", its row")
+
+
+@pytest.mark.parametrize("cache", CACHES)
+@pytest.mark.parametrize("decode", [False, True])
+def test_a_cap_at_a_tiny_scale(cache, decode):
+    """Queries of 2^40 at a scale of 2^-40: the scores of a plain call, half a cap large, whose
+    quotient of scale and cap leaves a polynomial's coefficients no place in fp32."""
+    say("tiny scale", cache, decode)
+    c = Call([20, 33], [1, 1] if decode else [20, 30], hq=4, hkv=2, d=128, cache=cache, softcap=30.0,
+             scale=128 ** -0.5 * 2.0 ** -40)
+    c.b.q = (c.b.q.float() * 2.0 ** 40).to(c.b.q.dtype)
+    c.q = c.b.q.cuda()
+    c.check(c.decode() if decode else c.prefill(), decode, f"{cache} tiny scale, decode {decode}")
