@@ -23,11 +23,8 @@ struct PlainScore {
   __device__ __forceinline__ const PlainScore& held() const { return *this; }
 };
 
-// The odd polynomials nearest to tanh in [0, 0.6] (off by 8e-8 of it) and [0, 0.5] (by 7e-7):
-// z + z^3 (c0 + c1 z^2 + ..).
-constexpr float kTanh4[4] = {-0.333326216f, 0.133135208f, -0.0522311078f, 0.0156404821f};
+// The odd polynomial nearest to tanh in [0, 0.5] (off by 7e-7 of it): z + z^3 (c0 + c1 z^2 + ..).
 constexpr float kTanh3[3] = {-0.333282646f, 0.132067148f, -0.0447894702f};
-
 // kTanh3 in y = 2 log2(e) z.
 constexpr float kTanhY[3] = {-0.0400316641f, 0.00190535828f, -7.76155430e-05f};
 
@@ -59,21 +56,12 @@ struct ModScore {
   }
 
   // cap tanh(dot scale / cap) as cap (1 - 2 / (e^2x + 1)), off by 2^-22 of the cap, which for
-  // one up to kSmallCap is 2^-14 of a weight; for a larger one, near zero, by kTanh4. kExact:
-  // the library's tanh.
+  // one up to kSmallCap is 2^-14 of a weight. kExact: the library's tanh.
   static constexpr float kSmallCap = 256.f;   // in the log2 domain
   static __device__ __forceinline__ float capped_far(float dot, float exp_scale, float cap_log2) {
     const float u = fast_exp2(dot * exp_scale);
     return fmaf(-2.f * cap_log2, __builtin_amdgcn_rcpf(u + 1.f), cap_log2);
   }
-  static __device__ __forceinline__ float capped_near(float z, float cap_log2) {
-    const float w = z * z;
-    float h = fmaf(w, kTanh4[3], kTanh4[2]);
-    h = fmaf(h, w, kTanh4[1]);
-    h = fmaf(h, w, kTanh4[0]);
-    return z * cap_log2 * fmaf(h, w, 1.f);
-  }
-
   // The one or the other by the product's size, where a cap is large: off by 2^-19 of the
   // score. In y = 2 log2(e) z, which the exponential takes, so that a prefill tile needs no
   // register more.
@@ -81,7 +69,7 @@ struct ModScore {
                                                       float scale_log2) {
     const float y = dot * exp_scale, w = y * y;
     const float h = fmaf(fmaf(w, kTanhY[2], kTanhY[1]), w, kTanhY[0]);
-    const float far = fmaf(-2.f * cap_log2, __builtin_amdgcn_rcpf(fast_exp2(y) + 1.f), cap_log2);
+    const float far = capped_far(dot, exp_scale, cap_log2);
     return fabsf(y) < kLog2e ? dot * scale_log2 * fmaf(h, w, 1.f) : far;
   }
 
@@ -108,16 +96,17 @@ struct ModScore {
       for (int e = 0; e < n; ++e) x[e] *= scale_log2;
     } else if constexpr (kExact) {
 #pragma unroll
-      for (int e = 0; e < n; ++e) x[e] = cap_log2 * tanhf(x[e] * tanh_scale);
+      for (int e = 0; e < n; ++e) {
+        // where tanh z is z to fp32, without the quotient of scale and cap, which may underflow
+        const float z = x[e] * tanh_scale, y = cap_log2 * tanhf(z);
+        x[e] = fabsf(z) < 0x1p-12f ? x[e] * scale_log2 : y;
+      }
     } else if (c <= kSmallCap) {
 #pragma unroll
       for (int e = 0; e < n; ++e) x[e] = capped_far(x[e], exp_scale, cap_log2);
     } else {
 #pragma unroll
-      for (int e = 0; e < n; ++e) {
-        const float z = x[e] * tanh_scale, far = capped_far(x[e], exp_scale, cap_log2);
-        x[e] = fabsf(z) < 0.6f ? capped_near(z, cap_log2) : far;
-      }
+      for (int e = 0; e < n; ++e) x[e] = capped_each(x[e], exp_scale, cap_log2, scale_log2);
     }
   }
 

@@ -6,7 +6,7 @@ import torch
 import oracle
 import paper_2608_23658_amd.kvattn as K
 from tests.gpu_helpers import f64, require_gpu, say
-from tests.scored_helpers import MODS, Call, assert_scored
+from tests.scored_helpers import MODS, Call, assert_scored, assert_scored_f32
 from tests.test_gpu_scored_decode import _poison
 
 pytestmark = pytest.mark.gpu
@@ -250,3 +250,18 @@ def test_a_cap_at_a_tiny_scale(cache, decode):
     c.b.q = (c.b.q.float() * 2.0 ** 40).to(c.b.q.dtype)
     c.q = c.b.q.cuda()
     c.check(c.decode() if decode else c.prefill(), decode, f"{cache} tiny scale, decode {decode}")
+
+
+@pytest.mark.parametrize("cache,d", [("bf16", 128), ("f32", 64), ("8bit", 64)])
+def test_a_cap_past_every_score_leaves_them(cache, d):
+    """scale / softcap below fp32's least value: the scores are those of no cap."""
+    say("decode, a cap of 1e38", cache)
+    c = Call([5, 300], [1, 1], hq=4, hkv=2, d=d, cache=cache, scale=1e-8, q_size=1e8)
+    (ref, weight), kw = c.expected(True), dict(softcap=1e38)
+    if cache == "f32":
+        assert_scored_f32(c.decode(**kw), ref, weight, 300, c.score_size(), "f32 decode")
+    else:
+        assert_scored(c.decode(**kw), ref, weight, cache, 0.0, f"{cache} decode")
+    if d == 128:
+        c = Call([60, 300], [30, 9], hq=4, hkv=2, d=d, cache=cache, scale=1e-8, q_size=1e8)
+        assert_scored(c.prefill(**kw), *c.expected(False), cache, 0.0, f"{cache} prefill")
