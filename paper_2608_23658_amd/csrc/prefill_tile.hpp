@@ -463,14 +463,16 @@ __device__ __forceinline__ void prefill_tile(
     // redo the step's exponentials against it. Rows that did not outgrow
     // theirs get the same values again.
     if (__builtin_amdgcn_ballot_w64(m_ref == -INFINITY || !(psum <= kPsumBound)) != 0) {
-      if constexpr (Score::kOn)   // finished, as the maximum needs them
-        if constexpr (Score::form == Form::kBias) {
-          // computed again here, not kept from the slots
-          asm volatile("" : "+v"(s_cur[0]), "+v"(s_cur[1]));
+      // with a bias the scores less the reference, as the slots computed them, and computed
+      // again here, not kept from there
+      float taken = 0.f;
+      if constexpr (Score::form == Form::kBias) {
+        taken = ref;
+        asm volatile("" : "+v"(s_cur[0]), "+v"(s_cur[1]), "+v"(taken));
 #pragma unroll
-          for (int e = 0; e < 32; ++e) s_cur[e / 16][e % 16] = less(e, 0.f);
-        }
-      auto of_finished = [&](float x, float r) __attribute__((always_inline)) {
+        for (int e = 0; e < 32; ++e) s_cur[e / 16][e % 16] = less(e, taken);
+      }
+      auto finished = [&](float x, float r) __attribute__((always_inline)) {
         if constexpr (!Score::kOn) return fmaf(x, how, -r);
         else if constexpr (Score::form == Form::kBias) return x - r;
         else return fmaf(x, how.by, -r);
@@ -483,7 +485,7 @@ __device__ __forceinline__ void prefill_tile(
       }
       float mx = max3f(mp0, mp1, mp1);
       mx = max3f(mx, __shfl_xor(mx, 32, kWave), mx);
-      const float tmax = of_finished(mx, 0.f);
+      const float tmax = finished(mx, -taken);
       const bool grow = tmax > m_ref + kLazyRescale;
       rescale = __builtin_amdgcn_ballot_w64(grow) != 0;
       const float nref = grow ? tmax : m_ref;
@@ -491,10 +493,11 @@ __device__ __forceinline__ void prefill_tile(
       m_ref = nref;
       ref = (nref == -INFINITY) ? 0.f : nref;
       psum = 0.f;
+      const float more = ref - taken;
 #pragma unroll
       for (int e = 0; e < 32; e += 2) {
-        pw[e / 2] = pack_bf16x2(fast_exp2(of_finished(s_cur[e / 16][e % 16], ref)),
-                                fast_exp2(of_finished(s_cur[e / 16][e % 16 + 1], ref)));
+        pw[e / 2] = pack_bf16x2(fast_exp2(finished(s_cur[e / 16][e % 16], more)),
+                                fast_exp2(finished(s_cur[e / 16][e % 16 + 1], more)));
         psum = dot2_bf16(pw[e / 2], kBf16OnePair, psum);
       }
     }

@@ -120,10 +120,10 @@ struct ModScore {
   // How the softmax finds a step's scores, with its reference r taken off.
   struct Step {
     float by;               // times this
-    float slope, first;     // kBias: the bias of element e is slope key_of(e) + first
+    float slope, ago;       // kBias: the bias of element e is slope (key_of(e) + ago)
     __device__ __forceinline__ float at(float dot, int e, float r) const {
       if constexpr (kForm == Form::kBias)
-        return fmaf(dot, by, fmaf(slope, (float)key_of(e), first - r));
+        return fmaf(dot, by, fmaf(slope, (float)key_of(e), fmaf(slope, ago, -r)));
       return fmaf(dot, by, -r);
     }
   };
@@ -178,12 +178,11 @@ struct ModScore {
       }
       return {1.f, 0.f, 0.f};
     } else {
-      const float first = slope_log2 * at_lane;
-      if (scale_log2 > 0.f) return {scale_log2, slope_log2, first};
+      if (scale_log2 > 0.f) return {scale_log2, slope_log2, at_lane};
       // masked scores are minus infinity before a scale above zero
 #pragma unroll
       for (int e = 0; e < 32; ++e) s[e / 16][e % 16] *= scale_log2;
-      return {1.f, slope_log2, first};
+      return {1.f, slope_log2, at_lane};
     }
   }
   // cap_log2 <= kSmallCap, compared by its bits each time: no mask is kept.

@@ -91,3 +91,19 @@ def test_chunks_that_keep_their_tiles_give_the_prompts_bits(cache, mods):
         assert torch.equal(part.view(torch.int16), whole[at:at + n].view(torch.int16)), (at, n)
         at += n
     assert at == 600
+
+
+@pytest.mark.parametrize("cache", ["bf16", "8bit"])
+@pytest.mark.parametrize("mods", [dict(bias=True), dict(bias=True, window=30000)])
+def test_a_biased_rows_bits_depend_on_itself(cache, mods):
+    """Rows whose scores make their wavefronts move the softmax's reference leave the others of
+    their tile their bits."""
+    say("biased bits", cache)
+    c = Call([40000], [64], hq=8, hkv=2, d=128, cache=cache, **mods)
+    # biases of hundreds where they matter, and steps that leave most rows' references alone
+    c.dev_slopes = torch.full((8,), -0.02, device="cuda")
+    want = c.prefill()
+    c.q[::2] *= 100
+    got = c.prefill()
+    assert not torch.equal(got[::2], want[::2])
+    assert torch.equal(got[1::2].view(torch.int16), want[1::2].view(torch.int16))
