@@ -520,7 +520,17 @@ def prefill_chunk_fp8(q: torch.Tensor, kv_layer, num_blocks: int, block_table: t
     return out
 
 
+def _require_ints(**named):
+    """ctypes cuts an integer that does not fit the library's to its low 32 bits. (Called where
+    one does not, or is negative, which the library refuses by itself.)"""
+    for name, x in named.items():
+        if not -(1 << 31) <= x < 1 << 31:
+            raise ValueError(f"{name} {x} does not fit 32 bits")
+
+
 def _scoring(softcap, slopes, window: int, num_q_heads: int):
+    if softcap and not ctypes.c_float(softcap).value:
+        raise ValueError(f"softcap {softcap} is zero in fp32, which is no cap")
     if slopes is None:
         return Scoring(softcap, None, window)
     if slopes.dtype != torch.float32 or slopes.shape != (num_q_heads,):
@@ -534,6 +544,9 @@ def _decode_scored(call, q, kv_layer, num_blocks, block_table, seq_lens, num_kv_
     _require_batch(B, block_table, seq_lens)
     _require_out(out, q)
     code = _dtype_code(q.dtype)
+    num_blocks, max_seq_len = int(num_blocks), int(max_seq_len)
+    if (window | num_blocks | max_seq_len) >> 31:
+        _require_ints(window=window, num_blocks=num_blocks, max_seq_len=max_seq_len)
     scoring = _scoring(softcap, slopes, window, Hq)
     _require_here(q, kv_layer, block_table, seq_lens, slopes, out, ws)
     if out is None:
@@ -542,9 +555,9 @@ def _decode_scored(call, q, kv_layer, num_blocks, block_table, seq_lens, num_kv_
         most = min(max_seq_len, window + 15) if window > 0 else max_seq_len
         ws = _made_for(stream, workspace, decode_workspace_bytes(B, Hq, d, most), q.device)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
-    check(call(q.data_ptr(), _ptr(kv_layer), int(num_blocks), block_table.data_ptr(),
+    check(call(q.data_ptr(), _ptr(kv_layer), num_blocks, block_table.data_ptr(),
                seq_lens.data_ptr(), out.data_ptr(), B, Hq, int(num_kv_heads), d, int(block_size),
-               int(block_table.shape[1]), int(max_seq_len), float(scale), scoring, code,
+               int(block_table.shape[1]), max_seq_len, float(scale), scoring, code,
                ws.data_ptr(), ws.numel(), _stream(stream)))
     return out
 
@@ -585,6 +598,11 @@ def _prefill_scored(call, q, kv_layer, num_blocks, block_table, seq_lens, cu_seq
     _require_rows(B, block_table, seq_lens, cu_seqlens_q)
     _require_out(out, q)
     code = _dtype_code(q.dtype)
+    num_blocks, max_seq_len = int(num_blocks), int(max_seq_len)
+    budget = T if max_num_batched_tokens is None else int(max_num_batched_tokens)
+    if (window | num_blocks | max_seq_len | budget) >> 31:
+        _require_ints(window=window, num_blocks=num_blocks, max_seq_len=max_seq_len,
+                      max_num_batched_tokens=budget)
     scoring = _scoring(softcap, slopes, window, Hq)
     _require_here(q, kv_layer, block_table, seq_lens, cu_seqlens_q, slopes, out, ws)
     if out is None:
@@ -592,10 +610,9 @@ def _prefill_scored(call, q, kv_layer, num_blocks, block_table, seq_lens, cu_seq
     if ws is None:
         ws = _made_for(stream, workspace, prefill_workspace_bytes(B, T, Hq, d), q.device)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
-    budget = T if max_num_batched_tokens is None else int(max_num_batched_tokens)
-    check(call(q.data_ptr(), _ptr(kv_layer), int(num_blocks), block_table.data_ptr(),
+    check(call(q.data_ptr(), _ptr(kv_layer), num_blocks, block_table.data_ptr(),
                seq_lens.data_ptr(), cu_seqlens_q.data_ptr(), out.data_ptr(), B, T, budget, Hq,
-               int(num_kv_heads), d, int(block_size), int(block_table.shape[1]), int(max_seq_len),
+               int(num_kv_heads), d, int(block_size), int(block_table.shape[1]), max_seq_len,
                float(scale), scoring, code, ws.data_ptr(), ws.numel(), _stream(stream)))
     return out
 
@@ -671,6 +688,9 @@ def _qkv_append(call, q, k, v, slot_mapping, kv_layer, num_blocks, positions, ro
              rope_table.dtype is torch.float32 and rope_table.dim() == 2)):
         _refuse_rows(q, k, v, slot_mapping, q_weight, k_weight, rope_table, positions)
     code = _dtype_code(dt)
+    num_blocks = int(num_blocks)
+    if num_blocks >> 31:
+        _require_ints(num_blocks=num_blocks)
     rope_len = rot = axes = pos = table = 0
     pairs = ()
     if rope_table is not None:
@@ -683,6 +703,8 @@ def _qkv_append(call, q, k, v, slot_mapping, kv_layer, num_blocks, positions, ro
             pairs = (rot // 2,)
         else:
             raise ValueError("several axes of positions need sections")
+        if any(p >> 31 for p in pairs):
+            _require_ints(**{f"section {i}": p for i, p in enumerate(pairs)})
         if len(pairs) != axes or axes > 4:
             raise ValueError(f"{axes} axes of positions, {len(pairs)} sections (at most 4)")
     elif positions is not None or sections is not None:
@@ -703,7 +725,7 @@ def _qkv_append(call, q, k, v, slot_mapping, kv_layer, num_blocks, positions, ro
                     0 if k_weight is None else k_weight.data_ptr(), eps, table, rope_len, rot,
                     bool(interleaved), pos, axes, pairs)
     check(call(q.data_ptr(), qs[0], k.data_ptr(), ks[0], v.data_ptr(), vs[0], prep,
-               slot_mapping.data_ptr(), out.data_ptr(), _ptr(kv_layer), int(num_blocks), T, Hq,
+               slot_mapping.data_ptr(), out.data_ptr(), _ptr(kv_layer), num_blocks, T, Hq,
                Hkv, d, int(block_size), code, _stream(stream)))
     return out
 

@@ -244,3 +244,68 @@ def test_made_for_the_current_stream_without_one(notes, name):  # noqa: F811
     CALLS[name]()
     assert notes.made and all(on == HERE.cuda_stream for _, on in notes.made)
     assert not notes.recorded
+
+
+# ---- what the binding hands to the library ----
+class _Asked(Exception):
+    pass
+
+
+def _asked(monkeypatch):
+    """Calls of the library end in _Asked, with its arguments."""
+    class Library:
+        def __getattr__(self, name):
+            def call(*a):
+                if name.endswith("bytes"):
+                    return 4096
+                raise _Asked(*a)
+            return call
+    monkeypatch.setattr(K, "lib", Library)
+    monkeypatch.setattr(K, "_require_here", lambda *ts: None)
+    monkeypatch.setattr(K, "_stream", lambda stream: 0)
+
+
+WIDE = [(1 << 32) + 5, 1 << 31, -(1 << 31) - 1, 1 << 64]
+
+
+@pytest.mark.parametrize("wide", WIDE)
+@pytest.mark.parametrize("name", sorted(n for n in CALLS if "scored" in n))
+def test_integers_past_32_bits_are_refused(monkeypatch, name, wide):
+    """ctypes would cut a window of 2^32 + 5 to one of 5."""
+    _asked(monkeypatch)
+    monkeypatch.setitem(SCORED, "window", wide)
+    with pytest.raises(ValueError, match="window .* 32 bits"):
+        CALLS[name]()
+    monkeypatch.setitem(SCORED, "window", 20)
+    monkeypatch.setitem(KW, "max_seq_len", wide)
+    with pytest.raises(ValueError, match="max_seq_len .* 32 bits"):
+        CALLS[name]()
+
+
+@pytest.mark.parametrize("name", sorted(n for n in CALLS if "scored" in n))
+def test_what_the_library_refuses_reaches_it(monkeypatch, name):
+    _asked(monkeypatch)
+    monkeypatch.setitem(SCORED, "window", -1)
+    with pytest.raises(_Asked) as e:
+        CALLS[name]()
+    scoring = next(x for x in e.value.args if isinstance(x, K.Scoring))
+    assert (scoring.softcap, scoring.window) == (30.0, -1)
+
+
+@pytest.mark.parametrize("name", sorted(n for n in CALLS if "scored" in n))
+def test_a_cap_that_fp32_rounds_to_zero_is_refused(monkeypatch, name):
+    _asked(monkeypatch)
+    monkeypatch.setitem(SCORED, "softcap", 1e-60)
+    with pytest.raises(ValueError, match="softcap"):
+        CALLS[name]()
+
+
+@pytest.mark.parametrize("name", ["qkv_append", "qkv_append_fp8"])
+def test_sections_and_blocks_past_32_bits_are_refused(monkeypatch, name):
+    _asked(monkeypatch)
+    q, k, v, slots, layer, _ = _qkv_args()
+    rope = dict(rope_table=torch.zeros(32, D), positions=_i32(2, T))
+    with pytest.raises(ValueError, match="section .* 32 bits"):
+        getattr(K, name)(q, k, v, slots, 0, 2, **rope, sections=((1 << 32) + 60, 4))
+    with pytest.raises(ValueError, match="num_blocks .* 32 bits"):
+        getattr(K, name)(q, k, v, slots, 0, (1 << 32) + 2)
