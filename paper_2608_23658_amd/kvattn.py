@@ -439,12 +439,23 @@ def _require_fp8_layer(kv_layer, num_blocks: int, num_kv_heads: int, head_dim: i
             raise ValueError(f"kv_layer has {have} bytes, {num_blocks} blocks need {need}")
 
 
-def _require_layer(kv_layer, num_blocks: int, num_kv_heads: int, head_dim: int, esz: int):
+def _require_layer(kv_layer, num_blocks: int, num_kv_heads: int, head_dim: int, dtype):
+    """A layer as a tensor is of the rows' type, or plain integers that hold its bytes."""
     if isinstance(kv_layer, torch.Tensor):
+        if kv_layer.dtype is not dtype and kv_layer.dtype.is_floating_point:
+            raise ValueError(f"kv_layer is {kv_layer.dtype}, the rows are {dtype}")
         have = kv_layer.numel() * kv_layer.element_size()
-        need = int(num_blocks) * 2 * num_kv_heads * 16 * head_dim * esz
+        need = int(num_blocks) * 2 * num_kv_heads * 16 * head_dim * dtype.itemsize
         if have < need:
             raise ValueError(f"kv_layer has {have} bytes, {num_blocks} blocks need {need}")
+
+
+def _require_layer8(kv_layer, num_blocks: int, num_kv_heads: int, head_dim: int):
+    """A layer in 8 bits as a tensor: e4m3, or plain integers."""
+    if isinstance(kv_layer, torch.Tensor) and kv_layer.dtype is not torch.float8_e4m3fn and \
+            kv_layer.dtype.is_floating_point:
+        raise ValueError(f"kv_layer is {kv_layer.dtype}, not one in 8 bits")
+    _require_fp8_layer(kv_layer, num_blocks, num_kv_heads, head_dim)
 
 
 def kv_append_fp8(k_new: torch.Tensor, v_new: torch.Tensor, slot_mapping: torch.Tensor, kv_layer,
@@ -570,7 +581,7 @@ def decode_scored(q: torch.Tensor, kv_layer, num_blocks: int, block_table: torch
                   stream=None) -> torch.Tensor:
     """``decode`` with other scores: capped at ``softcap`` by a tanh (0: not), biased by
     ``slopes`` [Hq] float32 times the distance, over the last ``window`` tokens (0: all)."""
-    _require_layer(kv_layer, num_blocks, num_kv_heads, q.shape[2], q.element_size())
+    _require_layer(kv_layer, num_blocks, num_kv_heads, q.shape[2], q.dtype)
     return _decode_scored(lib().kvattn_decode_scored, q, kv_layer, num_blocks, block_table,
                           seq_lens, num_kv_heads, max_seq_len, softcap, slopes, window, block_size,
                           scale, out, ws, stream)
@@ -583,7 +594,7 @@ def decode_scored_fp8(q: torch.Tensor, kv_layer, num_blocks: int, block_table: t
                       out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
                       stream=None) -> torch.Tensor:
     """``decode_scored`` over a layer in 8 bits: ``q`` [B, Hq, d] bf16."""
-    _require_fp8_layer(kv_layer, num_blocks, num_kv_heads, q.shape[2])
+    _require_layer8(kv_layer, num_blocks, num_kv_heads, q.shape[2])
     return _decode_scored(lib().kvattn_decode_scored_fp8, q, kv_layer, num_blocks, block_table,
                           seq_lens, num_kv_heads, max_seq_len, softcap, slopes, window, block_size,
                           scale, out, ws, stream)
@@ -625,7 +636,7 @@ def prefill_chunk_scored(q: torch.Tensor, kv_layer, num_blocks: int, block_table
                          out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
                          stream=None) -> torch.Tensor:
     """``prefill_chunk`` with the scores of ``decode_scored``: ``q`` [T, Hq, d] bf16."""
-    _require_layer(kv_layer, num_blocks, num_kv_heads, q.shape[2], q.element_size())
+    _require_layer(kv_layer, num_blocks, num_kv_heads, q.shape[2], q.dtype)
     return _prefill_scored(lib().kvattn_prefill_chunk_scored, q, kv_layer, num_blocks, block_table,
                            seq_lens, cu_seqlens_q, num_kv_heads, max_seq_len,
                            max_num_batched_tokens, softcap, slopes, window, block_size, scale, out,
@@ -641,7 +652,7 @@ def prefill_chunk_scored_fp8(q: torch.Tensor, kv_layer, num_blocks: int,
                              out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
                              stream=None) -> torch.Tensor:
     """``prefill_chunk_scored`` over a layer in 8 bits."""
-    _require_fp8_layer(kv_layer, num_blocks, num_kv_heads, q.shape[2])
+    _require_layer8(kv_layer, num_blocks, num_kv_heads, q.shape[2])
     return _prefill_scored(lib().kvattn_prefill_chunk_scored_fp8, q, kv_layer, num_blocks,
                            block_table, seq_lens, cu_seqlens_q, num_kv_heads, max_seq_len,
                            max_num_batched_tokens, softcap, slopes, window, block_size, scale, out,
@@ -743,7 +754,7 @@ def qkv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slot_mapping: 
     must lie together, tokens may lie apart. ``q_weight`` and ``k_weight`` [d]: RMS norm of
     each head. ``rope_table`` [positions, rot_dim] float32: cosines, then sines, looked up at
     ``positions`` [T] int32 or, with ``sections`` (pairs of each axis), [axes, T]."""
-    _require_layer(kv_layer, num_blocks, k.shape[1], k.shape[2], k.element_size())
+    _require_layer(kv_layer, num_blocks, k.shape[1], k.shape[2], k.dtype)
     return _qkv_append(lib().kvattn_qkv_append, q, k, v, slot_mapping, kv_layer, num_blocks,
                        positions, rope_table, sections, interleaved, q_weight, k_weight, eps, out,
                        block_size, stream)
@@ -758,7 +769,7 @@ def qkv_append_fp8(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slot_mappi
                    stream=None) -> torch.Tensor:
     """``qkv_append`` into a layer in 8 bits; tokens of one block must stand together in
     ``slot_mapping``."""
-    _require_fp8_layer(kv_layer, num_blocks, k.shape[1], k.shape[2])
+    _require_layer8(kv_layer, num_blocks, k.shape[1], k.shape[2])
     return _qkv_append(lib().kvattn_qkv_append_fp8, q, k, v, slot_mapping, kv_layer, num_blocks,
                        positions, rope_table, sections, interleaved, q_weight, k_weight, eps, out,
                        block_size, stream)

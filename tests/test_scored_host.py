@@ -309,3 +309,24 @@ def test_sections_and_blocks_past_32_bits_are_refused(monkeypatch, name):
         getattr(K, name)(q, k, v, slots, 0, 2, **rope, sections=((1 << 32) + 60, 4))
     with pytest.raises(ValueError, match="num_blocks .* 32 bits"):
         getattr(K, name)(q, k, v, slots, 0, (1 << 32) + 2)
+
+
+@pytest.mark.parametrize("name", sorted(CALLS))
+@pytest.mark.parametrize("dtype,right", [(torch.bfloat16, "own"), (torch.float32, None),
+                                         (torch.float16, None), (torch.float8_e4m3fn, "8bit"),
+                                         (torch.float8_e5m2, None), (torch.uint8, "both"),
+                                         (torch.int16, "both")])
+def test_a_layer_of_another_type_is_refused(monkeypatch, name, dtype, right):
+    """Rows in bf16 over a layer tensor in fp32, say, whose bytes would do."""
+    _asked(monkeypatch)
+    layer = torch.zeros(1 << 18, dtype=dtype)
+    if "qkv" in name:
+        args = _qkv_args()[:4] + (layer, 2)
+        kw = {}
+    else:
+        q, _, blocks, *rest = _batch()
+        args = (q, layer, blocks, *rest) + ((_i32(5),) if "prefill" in name else ())
+        kw = {**KW, **SCORED}
+    ok = right in ("both", "8bit" if name.endswith("fp8") else "own")
+    with pytest.raises(_Asked if ok else ValueError, match=None if ok else "kv_layer is"):
+        getattr(K, name)(*args, **kw)
