@@ -735,7 +735,9 @@ def _qkv_append(call, q, k, v, slot_mapping, kv_layer, num_blocks, positions, ro
     prep = NormRope(0 if q_weight is None else q_weight.data_ptr(),
                     0 if k_weight is None else k_weight.data_ptr(), eps, table, rope_len, rot,
                     bool(interleaved), pos, axes, pairs)
-    check(call(q.data_ptr(), qs[0], k.data_ptr(), ks[0], v.data_ptr(), vs[0], prep,
+    # (one token's stride is any number)
+    far = (qs[0], ks[0], vs[0]) if T > 1 else (Hq * d, Hkv * d, Hkv * d)
+    check(call(q.data_ptr(), far[0], k.data_ptr(), far[1], v.data_ptr(), far[2], prep,
                slot_mapping.data_ptr(), out.data_ptr(), _ptr(kv_layer), num_blocks, T, Hq,
                Hkv, d, int(block_size), code, _stream(stream)))
     return out

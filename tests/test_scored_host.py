@@ -330,3 +330,18 @@ def test_a_layer_of_another_type_is_refused(monkeypatch, name, dtype, right):
     ok = right in ("both", "8bit" if name.endswith("fp8") else "own")
     with pytest.raises(_Asked if ok else ValueError, match=None if ok else "kv_layer is"):
         getattr(K, name)(*args, **kw)
+
+
+@pytest.mark.parametrize("name", ["qkv_append", "qkv_append_fp8"])
+def test_one_tokens_stride_does_not_count(monkeypatch, name):
+    """torch gives a dimension of one any stride: a row that was a column's, say."""
+    _asked(monkeypatch)
+    q, k, v = (torch.zeros(h, D, 1, dtype=torch.bfloat16).permute(2, 0, 1) for h in (HQ, HKV, HKV))
+    assert q.is_contiguous() and q.stride(0) == 1
+    with pytest.raises(_Asked) as e:
+        getattr(K, name)(q, k, v, _i32(1), torch.zeros(1 << 17, dtype=torch.uint8), 2)
+    assert [e.value.args[i] for i in (1, 3, 5)] == [HQ * D, HKV * D, HKV * D]
+    q = torch.zeros(T, HQ + 4, D, dtype=torch.bfloat16)[:, :HQ]
+    with pytest.raises(_Asked) as e:
+        getattr(K, name)(q, *_rows()[1:], _i32(T), torch.zeros(1 << 17, dtype=torch.uint8), 2)
+    assert e.value.args[1] == (HQ + 4) * D
