@@ -14,12 +14,18 @@
 // Each kind of scores has kernels of its own, since one that asks for its kind at every score
 // needs more registers than there are and spilled. Per call, plain prefill / window of 1024 /
 // bias / cap / cap and bias (32 query heads over 8):
-//   8192 rows over 24576                    3447 /  222 / 3254 / 4355 / 4210 us
-//   4096 rows over 12288                     909 /  115 /  831 / 1115 / 1073 us
-//   201 rows over 6150                      51.1 / 42.0 / 50.9 / 62.6 / 59.3 us
+//   8192 rows over 24576                    3429 /  207 / 3278 / 4279 / 4311 us
+//   the same over 8 bits                    3386 /  194 / 3289 / 4276 / 4259 us
+//   4096 rows over 12288                     884 /  106 /  854 / 1102 / 1096 us
+//   201 rows over 6150                      49.3 / 36.7 / 52.5 / 61.7 / 59.4 us
 //   2048 rows over 6144 and 64 of 1024 to
-//     8192, 8 bits                           347 /   78 /  343 /  426 /  424 us
+//     8192, 8 bits                           360 /   82 /  362 /  437 /  426 us
 // (the biased ones gain by the order of the keys: near ones hold a row's largest scores.)
+// A narrow window leaves most of a call to what a tile has beside its steps: 8192 rows over
+// 24576 take 91, 140, 203 and 573 us under windows of 128, 512, 1024 and 4096, 34, 60, 120 and
+// 479 of them matrix work that the rows see. The tile map (10 us) comes first, a tile's start,
+// first gathers and output are about 6 us with nothing beside them, and each of a tile's
+// wavefronts multiplies all of its steps, masked where its 32 rows see none of one.
 
 #pragma once
 

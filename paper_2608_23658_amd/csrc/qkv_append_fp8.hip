@@ -2,9 +2,9 @@
 // are scaled and rounded from the fp32 values that the rotation gives. One launch: the
 // first workgroups append K and V as append_fp8.hpp does, the others have the q rows. A K
 // row is normed and rotated in the lanes that hold it for its scale.
-// 8192 tokens in order, 32 query heads over 8 of 128, bf16, inputs not in a cache: 53.6 us, where
-// copying as many bytes takes 38.5; 4096 tokens of 64 over 8: 39.7, copy 32.9, and 36.5 in a
-// graph. With K's pairs looked up value by value it was 93.8 and 73.6. 256 scattered tokens: 16.2 us
+// 8192 tokens in order, 32 query heads over 8 of 128, bf16, inputs not in a cache: 53.5 us, where
+// copying as many bytes takes 38.5; 4096 tokens of 64 over 8: 39.5, copy 32.9, and 35.1 in calls
+// one after another. With K's pairs looked up value by value it was 93.8 and 73.6. 256 scattered tokens: 16.2 us
 // (25.4), a chain of latencies: slots, exponents and positions, rows and table, codes.
 
 #include "append_fp8.hpp"

@@ -247,9 +247,9 @@ __device__ __forceinline__ void q_rows(const QkvArgs& a, int wg, int groups, int
 }
 
 // How rows are dealt to wavefronts: more heads to each where there are enough to fill the
-// card anyway. 8192 / 2048 tokens, 32 query heads over 8: at these bounds 43.5 / 19.2 us, at half
-// of them 43.5 / 18.5 (but 1777 tokens of 12 over 3 in fp32 8.2 instead of 7.4), at twice
-// 42.0 / 20.9 (4096 tokens of 64 over 8, 8 bits, 39.2 instead of 36.4). Then as many to each of a
+// card anyway. 8192 / 2048 tokens, 32 query heads over 8: at these bounds 39.9 / 17.1 us, at half
+// of them 39.9 / 16.4 (but 1777 tokens of 12 over 3 in fp32 9.6 instead of 9.3), at twice
+// 38.8 / 19.1 (4096 tokens of 64 over 8, 8 bits, 42.2 instead of 39.5). Then as many to each of a
 // workgroup's wavefronts (46 heads over 1: 46.2 -> 42.0 us).
 struct QkvSplit {
   int per_wave, groups;   // heads of a wavefront, workgroups of a run
