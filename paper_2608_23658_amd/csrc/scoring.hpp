@@ -2,6 +2,7 @@
 // cut to a window.
 #pragma once
 
+#include <algorithm>
 #include <cmath>
 
 #include "common.hpp"
@@ -224,8 +225,17 @@ ModScore<kForm> mod_score(float scale, const ScoreMods& m) {
   s.p1 = s.p0 * w * kTanh3[0];
   s.p2 = s.p0 * w * w * kTanh3[1];
   s.p3 = s.p0 * w * w * w * kTanh3[2];
-  // none is near where a coefficient has left fp32's normal range (a tiny cap, a tiny scale)
-  s.near = w < 1e9f && std::isnormal(s.p3) ? 0.5f / std::fabs(s.tanh_scale) : 0.f;
+  // A coefficient below fp32's normal range (a tiny scale, a large cap) is left out, and what is
+  // near ends where its term would be 2^-22 of the score.
+  float z = 0.5f;
+  if (!std::isnormal(s.p3)) z = 0.13f;
+  if (!std::isnormal(s.p2)) z = 0.036f;
+  if (!std::isnormal(s.p1)) z = 8e-4f;
+  // past the range none is near (a tiny cap), nor are products whose squares are
+  s.near = w < 1e9f && std::isfinite(s.p3) ? std::min(z / std::fabs(s.tanh_scale), 1.8e19f) : 0.f;
+  if (z < 0.5f) s.p3 = 0.f;
+  if (z < 0.13f) s.p2 = 0.f;
+  if (z < 0.036f) s.p1 = 0.f;
   return s;
 }
 

@@ -245,8 +245,8 @@ def test_a_cap_at_a_tiny_scale(cache, decode):
     """Queries of 2^40 at a scale of 2^-40: the scores of a plain call, half a cap large, whose
     quotient of scale and cap leaves a polynomial's coefficients no place in fp32."""
     say("tiny scale", cache, decode)
-    c = Call([20, 33], [1, 1] if decode else [20, 30], hq=4, hkv=2, d=128, cache=cache, softcap=30.0,
-             scale=128 ** -0.5 * 2.0 ** -40)
+    c = Call([20, 33], [1, 1] if decode else [20, 30], hq=4, hkv=2, d=128, cache=cache,
+             softcap=30.0, scale=128 ** -0.5 * 2.0 ** -40)
     c.b.q = (c.b.q.float() * 2.0 ** 40).to(c.b.q.dtype)
     c.q = c.b.q.cuda()
     c.check(c.decode() if decode else c.prefill(), decode, f"{cache} tiny scale, decode {decode}")
@@ -265,3 +265,18 @@ def test_a_cap_past_every_score_leaves_them(cache, d):
     if d == 128:
         c = Call([60, 300], [30, 9], hq=4, hkv=2, d=d, cache=cache, scale=1e-8, q_size=1e8)
         assert_scored(c.prefill(**kw), *c.expected(False), cache, 0.0, f"{cache} prefill")
+
+
+@pytest.mark.parametrize("cache", CACHES)
+@pytest.mark.parametrize("shift", [10, 15, 20, 30, 60, 100])
+@pytest.mark.parametrize("q_size", [4.0, 1.0, 0.25, 2.0 ** -9])
+def test_caps_at_scales_that_leave_a_polynomial_fewer_terms(cache, shift, q_size):
+    """Queries of 2^shift at a scale of 2^-shift: the coefficients of a step of small products
+    leave fp32 one after another, and with them the products that are taken as small, down from
+    half the cap; at the last shifts the products' squares leave it too."""
+    say("prefill scales", cache, shift, q_size)
+    c = Call([20, 33, 300], [20, 30, 70], hq=4, hkv=2, d=128, cache=cache, softcap=30.0,
+             q_size=q_size, scale=128 ** -0.5 * 2.0 ** -shift)
+    c.b.q = (c.b.q.float() * 2.0 ** shift).to(c.b.q.dtype)
+    c.q = c.b.q.cuda()
+    c.check(c.prefill(), False, f"{cache} 2^-{shift} {q_size}")
