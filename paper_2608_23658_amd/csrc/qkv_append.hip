@@ -78,8 +78,9 @@ __device__ __forceinline__ void kv_rows(const QkvArgs& a, int k, int h0, int h1,
       tok[r] = kRunTokens * (k - 1) + __shfl(packed, i16, kWave);
     }
     auto load = [&](int h, uint4 (&x)[kN]) __attribute__((always_inline)) {
-      const uint8_t* src = (h < hkv ? k_rows : v_rows) + (size_t)(h < hkv ? h : h - hkv) * (D * ESZ);
-      const size_t stride = h < hkv ? k_stride : v_stride;
+      const bool is_k = h < hkv;
+      const uint8_t* src = (is_k ? k_rows : v_rows) + (size_t)(is_k ? h : h - hkv) * (D * ESZ);
+      const size_t stride = is_k ? k_stride : v_stride;
       // addresses are made here: kept over the heads, one for each stride, they took the third
       // wavefront of a SIMD (178 registers instead of 168)
       int at = piece;
@@ -90,8 +91,8 @@ __device__ __forceinline__ void kv_rows(const QkvArgs& a, int k, int h0, int h1,
         asm volatile("" : "+v"(t));
 #pragma unroll
         for (int p = 0; p < R::kPer; ++p)
-          x[r * R::kPer + p] =
-              load_nt(reinterpret_cast<const uint4*>(src + (size_t)t * stride) + at + R::kLanes * p);
+          x[r * R::kPer + p] = load_nt(reinterpret_cast<const uint4*>(src + (size_t)t * stride) +
+                                       at + R::kLanes * p);
       }
     };
     uint4 ahead[kN];

@@ -85,8 +85,8 @@ def test_decode(seed):
     _give_up(c, lens, new)
     loose = int(rng.integers(0, 3)) * 1000
     need = (c.b.max_seq_len + loose) // 16 + 1
-    c.b.block_table = np.pad(c.b.block_table, ((0, 0), (0, max(0, need - c.b.block_table.shape[1]))),
-                             constant_values=-1)
+    short = max(0, need - c.b.block_table.shape[1])
+    c.b.block_table = np.pad(c.b.block_table, ((0, 0), (0, short)), constant_values=-1)
     c.set_table()
     _check(c, c.decode(max_seq_len=c.b.max_seq_len + loose), True, what)
 
